@@ -20,88 +20,12 @@
 #include "dctmm.cuh"
 #include "attend.cuh"
 #include "prefill.cuh"
+#include "ctx.cuh"
 
 using namespace freqkv;
 
-struct freqkv_ctx {
-    int device = 0;
-    int sm_count = 0;
-    freqkv_variant forced = FREQKV_AUTO;
-    std::map<std::tuple<int32_t, int32_t, int32_t>, Basis> bases;  // (n_in, n_keep, first retained component)
-    std::map<std::pair<int32_t, int32_t>, FdctPlan> fdct_plans;
-    // keys: (n_in, n_keep, family of factorisation asked for: 0 = the kernel's own choice)
-    std::map<std::tuple<int32_t, int32_t, int32_t>, DctmmPlan> dctmm_plans;
-    std::map<std::tuple<int32_t, int32_t, int32_t>, bool> dctmm_fits;  // does a factorisation meet the kernel's limits
-    int32_t fast_family = 0;
-    size_t basis_bytes = 0;
-    void* scratch = nullptr;
-    size_t scratch_bytes = 0;
-    int32_t* status_dev = nullptr;
-    GemmState gemm;
-    std::string last_error;
-    // Work areas (folded rows, far sums, staging, attention partials) are shared by all calls on this
-    // context: a call on another stream than the previous one first waits for that one's work.
-    cudaEvent_t work_done = nullptr;
-    cudaStream_t work_stream = nullptr;
-    bool work_recorded = false;
-    // instrumentation
-    bool timing = false;
-    std::vector<std::pair<cudaEvent_t, cudaEvent_t>> pending, spare;
-    int64_t kernels_launched = 0;
-    // host-buffer entry point: device staging caches
-    void* stage[2] = {nullptr, nullptr};
-    size_t stage_bytes = 0;
-    // decode attention: RoPE table of one base, partial results of the row splits
-    float2* rope_table = nullptr;
-    int32_t rope_rows = 0;
-    double rope_base = 0.0;
-    void* attend_work = nullptr;  // attend_ticket_bytes of tickets, then the splits' partials
-    size_t attend_work_bytes = 0;
-    int32_t* attend_lens = nullptr;  // host: the last call's lengths; what else its split of the rows follows from; that split
-    int32_t attend_lens_room = 0, attend_key[4] = {0, 0, 0, 0};
-    AttendPlan attend_last = {};
-    bool attend_tickets_clear = false;  // zeroed on a stream that later calls are ordered behind
-    void* prefill_keys = nullptr;     // rotated keys of one layer, fp16
-    size_t prefill_keys_bytes = 0;
-    void* prefill_queries = nullptr;  // rotated, scaled queries of one chunk, fp16
-    size_t prefill_queries_bytes = 0;
-    cudaStream_t pipe[3] = {nullptr, nullptr, nullptr};  // copy in, compress, copy out
-    cudaEvent_t pipe_begin = nullptr, pipe_end = nullptr;
-    std::vector<cudaEvent_t> pipe_events;                // per group: copied in, compressed
-};
-
-namespace {
-
-constexpr size_t kScratchChunkBytes = size_t(1) << 30;  // per-chunk output staging of the scratch paths
-constexpr int32_t kDctRows = -1;  // plan key of the plain DCT matrix (power spectrum) among the retained-band offsets
-constexpr size_t kBasisBudgetBytes = size_t(12) << 30;  // plan cache is flushed beyond this
-constexpr size_t kAttendWorkBytes = size_t(16) << 20;   // decode attention: a work area that grows, grows ahead of need up to this
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true, changed = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev == dev) return;
-        changed = true;
-        if (cudaSetDevice(dev) != cudaSuccess) ok = false;
-    }
-    ~DeviceGuard()
-    {
-        if (changed) cudaSetDevice(prev);
-    }
-};
-
-// Orders the calls that use the context's work areas: on entry the caller's stream waits for the
-// previous such call if that one ran on a different stream; on exit the end of this call's work
-// is recorded.  (Calls on one stream are ordered anyway and pay nothing.)
-struct WorkOrder {
-    freqkv_ctx* ctx;
-    cudaStream_t stream;
-    WorkOrder(freqkv_ctx* c, cudaStream_t s);
-    ~WorkOrder();
-};
+// ---- what ctx.cuh declares ----
+namespace freqkv {
 
 freqkv_status cuda_fail(freqkv_ctx* ctx, cudaError_t e, const char* where)
 {
@@ -110,11 +34,15 @@ freqkv_status cuda_fail(freqkv_ctx* ctx, cudaError_t e, const char* where)
     return e == cudaErrorMemoryAllocation ? FREQKV_ERR_ALLOC : FREQKV_ERR_CUDA;
 }
 
-#define FREQKV_CUDA(ctx, call)                                             \
-    do {                                                                   \
-        const cudaError_t e__ = (call);                                    \
-        if (e__ != cudaSuccess) return cuda_fail((ctx), e__, #call);       \
-    } while (0)
+bool is_capturing(cudaStream_t stream)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(stream, &status) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return status != cudaStreamCaptureStatusNone;
+}
 
 WorkOrder::WorkOrder(freqkv_ctx* c, cudaStream_t s) : ctx(c), stream(s)
 {
@@ -181,6 +109,39 @@ freqkv_status check_tensors(const freqkv_layout& l, const void* k, const void* v
     if (a < b + bytes && b < a + bytes) return FREQKV_ERR_INVALID_ARG;  // K and V overlap
     return FREQKV_OK;
 }
+
+// The context's cos/sin table for `rope_base`, built on `stream` when the base or the capacity has
+// changed; *table stays null when RoPE is off.
+freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base, cudaStream_t stream, const float2** table)
+{
+    *table = nullptr;
+    if (!(rope_base > 0.f)) return FREQKV_OK;
+    if (!ctx->rope_table || ctx->rope_rows < capacity || ctx->rope_base != (double)rope_base) {
+        if (ctx->rope_table) {
+            FREQKV_CUDA(ctx, cudaDeviceSynchronize());  // an enqueued launch may still read the old table
+            cudaFree(ctx->rope_table);
+            ctx->rope_table = nullptr;
+        }
+        const int32_t rows = std::max(capacity, 2);
+        FREQKV_CUDA(ctx, cudaMalloc(&ctx->rope_table, (size_t)rows * 64 * sizeof(float2)));
+        const cudaError_t e = launch_rope_table(ctx->rope_table, rows, (double)rope_base, stream);
+        if (e != cudaSuccess) return cuda_fail(ctx, e, "rope_table");
+        ctx->rope_rows = rows;
+        ctx->rope_base = (double)rope_base;
+        ctx->kernels_launched += 1;
+    }
+    *table = ctx->rope_table;
+    return FREQKV_OK;
+}
+
+}  // namespace freqkv
+
+namespace {
+
+constexpr size_t kScratchChunkBytes = size_t(1) << 30;  // per-chunk output staging of the scratch paths
+constexpr int32_t kDctRows = -1;  // plan key of the plain DCT matrix (power spectrum) among the retained-band offsets
+constexpr size_t kBasisBudgetBytes = size_t(12) << 30;  // plan cache is flushed beyond this
+constexpr size_t kAttendWorkBytes = size_t(16) << 20;   // decode attention: a work area that grows, grows ahead of need up to this
 
 CacheView make_view(const freqkv_layout& l, void* k, void* v, int32_t batch0, int32_t batch_count)
 {
@@ -256,18 +217,6 @@ bool one_pass_heads(freqkv_ctx* ctx, const freqkv_layout& l, int32_t n_in, int32
 {
     return ctx->forced == FREQKV_AUTO && ctx->fast_family == 0 && l.dtype == FREQKV_BF16 && (l.head_dim == 64 || l.head_dim == 256) &&
            !gemm_is_direct(n_keep) && triples * (l.head_dim / 4) > ctx->sm_count && dctmm_applicable(ctx, l, n_in, n_keep);
-}
-
-// A captured call keeps the fast transform, whose kernel reads nothing but its plan: a capture may not allocate, and a later, larger
-// call would move the one-pass kernel's work area away under the replays.
-bool is_capturing(cudaStream_t stream)
-{
-    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(stream, &status) != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    return status != cudaStreamCaptureStatusNone;
 }
 
 void free_bases(freqkv_ctx* ctx)
@@ -476,38 +425,6 @@ freqkv_status get_scratch(freqkv_ctx* ctx, size_t bytes, void** out)
     return FREQKV_OK;
 }
 
-struct TransformTimer {
-    freqkv_ctx* ctx;
-    cudaStream_t stream;
-    std::pair<cudaEvent_t, cudaEvent_t> ev{nullptr, nullptr};
-    TransformTimer(freqkv_ctx* c, cudaStream_t s) : ctx(c), stream(s) { begin(); }
-    TransformTimer(freqkv_ctx* c, cudaStream_t s, bool start_now) : ctx(c), stream(s)
-    {
-        if (start_now) begin();
-    }
-    void begin()
-    {
-        if (!ctx->timing) return;
-        if (!ctx->spare.empty()) {
-            ev = ctx->spare.back();
-            ctx->spare.pop_back();
-        } else if (cudaEventCreate(&ev.first) != cudaSuccess || cudaEventCreate(&ev.second) != cudaSuccess) {
-            ev = {nullptr, nullptr};
-            cudaGetLastError();
-            return;
-        }
-        cudaEventRecord(ev.first, stream);
-    }
-    void end()
-    {
-        if (!ev.first) return;
-        cudaEventRecord(ev.second, stream);
-        ctx->pending.push_back(ev);
-        ev = {nullptr, nullptr};
-    }
-    ~TransformTimer() { end(); }
-};
-
 // Compress `count` sequences starting at batch0, all with the same (n_in, n_keep).  `of_triples`: the triples of the whole call where
 // this is a part of it that has to come out as the whole would (0: this is all of it).
 freqkv_status compress_group(freqkv_ctx* ctx, const freqkv_layout& l, void* k, void* v, int32_t batch0,
@@ -518,6 +435,8 @@ freqkv_status compress_group(freqkv_ctx* ctx, const freqkv_layout& l, void* k, v
     const CacheView view = make_view(l, k, v, batch0, batch_count);
     const int32_t n_mat = 2 * view.mats_per_tensor;
 
+    // A captured call keeps the fast transform, whose kernel reads nothing but its plan: a capture may not allocate, and a later, larger
+    // call would move the one-pass kernel's work area away under the replays.
     if (variant == FREQKV_FDCT && first == 0 && one_pass_heads(ctx, l, n_in, n_keep, of_triples ? of_triples : view.mats_per_tensor) &&
         !is_capturing(stream)) {
         const freqkv_status st = compress_group(ctx, l, k, v, batch0, batch_count, n_in, n_keep, sink, FREQKV_GEMM, stream);
@@ -1116,30 +1035,6 @@ freqkv_status freqkv_compress_host(freqkv_ctx* ctx, const freqkv_layout* layout,
         FREQKV_CUDA(ctx, cudaStreamWaitEvent(stream, ctx->pipe_end, 0));
     }
     return run;
-}
-
-// The context's cos/sin table for `rope_base`, built on `stream` when the base or the capacity has
-// changed; *table stays null when RoPE is off.
-static freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base, cudaStream_t stream, const float2** table)
-{
-    *table = nullptr;
-    if (!(rope_base > 0.f)) return FREQKV_OK;
-    if (!ctx->rope_table || ctx->rope_rows < capacity || ctx->rope_base != (double)rope_base) {
-        if (ctx->rope_table) {
-            FREQKV_CUDA(ctx, cudaDeviceSynchronize());  // an enqueued launch may still read the old table
-            cudaFree(ctx->rope_table);
-            ctx->rope_table = nullptr;
-        }
-        const int32_t rows = std::max(capacity, 2);
-        FREQKV_CUDA(ctx, cudaMalloc(&ctx->rope_table, (size_t)rows * 64 * sizeof(float2)));
-        const cudaError_t e = launch_rope_table(ctx->rope_table, rows, (double)rope_base, stream);
-        if (e != cudaSuccess) return cuda_fail(ctx, e, "rope_table");
-        ctx->rope_rows = rows;
-        ctx->rope_base = (double)rope_base;
-        ctx->kernels_launched += 1;
-    }
-    *table = ctx->rope_table;
-    return FREQKV_OK;
 }
 
 freqkv_status freqkv_check_attend(const freqkv_layout* layout, const void* k, const void* v, int32_t layer, const void* q,
