@@ -81,6 +81,29 @@ typedef struct {
     int64_t stride_batch, stride_layer, stride_head, stride_token;
 } freqkv_layout;
 
+/* ---- a cache in 8 bits ----
+ *
+ * K and V as 8-bit codes, each matrix cut into blocks of `block_tokens` consecutive rows (block i: rows [i * block_tokens,
+ * (i + 1) * block_tokens)) with one fp32 scale each; a value is  code * scale.  A cache takes half the memory of a bf16 one, and
+ * attention over it reads half the bytes.  With a = the largest finite magnitude of the rows that enter a block at once:
+ *   INT8  codes are integers in [-127, 127]; scale = a / 127 rounded to fp32, at least 2^-126 (0 for a = 0);
+ *         code = value / scale rounded to the nearest integer, ties to even;
+ *   E4M3  codes are 8-bit floating values (4 exponent bits, 3 mantissa bits, largest 448, no infinities); scale = the smallest
+ *         power of two with a <= 448 * scale, at least 2^-126 (0 for a = 0); code = value / scale rounded to nearest, ties to even.
+ * Infinities become the largest code of their sign; NaN stays NaN in E4M3 and becomes 0 in INT8.
+ * INT8 has the finer step where a block's values are of one size, E4M3 where a few channels are far larger than the others. */
+typedef enum { FREQKV_Q8_E4M3 = 0, FREQKV_Q8_INT8 = 1 } freqkv_q8_kind;
+
+/* Layout of the codes of ONE tensor (K or V; both must share it): code (b, l, h, t, c) lives at byte
+ * base + b*stride_batch + l*stride_layer + h*stride_head + t*stride_token + c.  Requirements: head_dim a multiple of 16 and at
+ * most 256, block_tokens 16, 32, 64 or 128, strides multiples of 16 under the rules of freqkv_layout, base 16-byte aligned.
+ * The scales of each tensor are a dense fp32 array [batch, layers, kv_heads, ceil(capacity / block_tokens)]. */
+typedef struct {
+    int32_t kind; /* freqkv_q8_kind */
+    int32_t batch, layers, kv_heads, capacity /* tokens */, head_dim, block_tokens;
+    int64_t stride_batch, stride_layer, stride_head, stride_token;
+} freqkv_q8_layout;
+
 typedef struct freqkv_ctx freqkv_ctx; /* opaque: projection bases, twiddles, scratch, status word */
 
 /* Fill `out` with the dense row-major [batch, layers, kv_heads, capacity, head_dim] layout. */
@@ -282,6 +305,28 @@ freqkv_status freqkv_attend_prefill(freqkv_ctx* ctx, const freqkv_layout* layout
                                     int32_t layer, const void* q, void* out, int32_t q_heads_per_kv, int32_t n_new,
                                     const int32_t* lens, float rope_base, float scale, void* cuda_stream);
 
+/* Append n_new incoming tokens to every sequence of an 8-bit cache.  new_k / new_v as for freqkv_append, of type `dtype`
+ * (FREQKV_BF16 or FREQKV_F32); rows [lens[b], lens[b] + n_new) of sequence b are written and lens[b] (host) grows by n_new.
+ * Rows that enter a block which holds rows already keep its scale where the scale of their own (above) is no larger; else the
+ * scale grows to that and the block's older codes become  code * old scale / new scale,  rounded again as above (in E4M3 that is exact but
+ * for codes that become subnormal).  Nothing else is written.  Same errors as freqkv_append, CAPACITY included; UNSUPPORTED for the rules of freqkv_q8_layout. */
+freqkv_status freqkv_append_q8(freqkv_ctx* ctx, const freqkv_q8_layout* layout, void* k, void* v, float* k_scale, float* v_scale,
+                               const void* new_k, const void* new_v, freqkv_dtype dtype, int32_t n_new, int32_t* lens,
+                               void* cuda_stream);
+
+/* Rows [0, lens[b]) of every matrix of a bf16 or fp32 cache (`src`, k_src, v_src) into an 8-bit cache, replacing what its first
+ * lens[b] rows held (the last block's rows from lens[b] on keep their codes, its scale is the new one).  Both layouts share batch,
+ * layers, kv_heads and head_dim; lens[b] in [0, both capacities].  With freqkv_dequantize this is how an 8-bit cache is compressed:
+ * out, freqkv_compress, in.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+freqkv_status freqkv_quantize(freqkv_ctx* ctx, const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
+                              const freqkv_q8_layout* layout, void* k, void* v, float* k_scale, float* v_scale, void* cuda_stream);
+
+/* The other way: rows [0, lens[b]) of a bf16 or fp32 cache <- code * scale, rounded once to its type.  The 8-bit cache is only
+ * read, nothing else of the other one is written.  Same rules and errors as freqkv_quantize. */
+freqkv_status freqkv_dequantize(freqkv_ctx* ctx, const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                const float* v_scale, const int32_t* lens, const freqkv_layout* dst, void* k_dst, void* v_dst,
+                                void* cuda_stream);
+
 /* Instrumentation for benchmarks.  With timing enabled every compression records a CUDA event
  * pair on the caller's stream around its transform kernel (the projection / fast-transform
  * launch, not the copy-back or table builders; the folded fp32 product's three launches together).  freqkv_get_timing waits for the recorded
@@ -356,6 +401,14 @@ freqkv_status freqkv_check_attend(const freqkv_layout* layout, const void* k, co
 freqkv_status freqkv_check_attend_prefill(const freqkv_layout* layout, const void* k, const void* v, int32_t layer,
                                           const void* q, const void* out, int32_t q_heads_per_kv, int32_t n_new,
                                           const int32_t* lens);
+
+freqkv_status freqkv_check_append_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                     const float* v_scale, const void* new_k, const void* new_v, freqkv_dtype dtype, int32_t n_new,
+                                     const int32_t* lens);
+/* (of freqkv_quantize and freqkv_dequantize alike) */
+freqkv_status freqkv_check_quantize(const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
+                                    const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                    const float* v_scale);
 
 /* Host-only diagnostic of the fast transform's plan (no device, no context): applies the
  * factored chain the FDCT variant would run for (n_in, n_keep) -- same factor choice, same

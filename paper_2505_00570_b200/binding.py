@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libfreqkv.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CAPACITY, ERR_ALLOC, ERR_CUDA, ERR_TIMEOUT = range(7)
 BF16, F32 = 0, 1
 AUTO, GEMM, FDCT, SIMT = 0, 1, 2, 3
+Q8_E4M3, Q8_INT8 = 0, 1   # codes of an 8-bit cache (freqkv_q8_kind)
 COOLEY_TUKEY, PRIME_FACTOR = 1, 2   # families of the bf16 fast transform (freqkv_set_fast_family)
 VARIANT_NAMES = {AUTO: "auto", GEMM: "gemm", FDCT: "fdct", SIMT: "simt"}
 
@@ -32,6 +33,7 @@ EXPORTS = [
     "freqkv_attend_prefill", "freqkv_check_attend_prefill",
     "freqkv_decode_graph_create", "freqkv_decode_graph_launch", "freqkv_decode_graph_destroy",
     "freqkv_set_wait_limit", "freqkv_selftest_bounded_wait", "freqkv_fast_plan_apply_host", "freqkv_set_fast_family", "freqkv_gemm_fold_levels", "freqkv_gemm_blocks",
+    "freqkv_append_q8", "freqkv_quantize", "freqkv_dequantize", "freqkv_check_append_q8", "freqkv_check_quantize",
 ]
 NOALLOC_MAX_BASIS_ELEMS = 1 << 20
 NOALLOC_STAGING_BYTES = 4 << 20
@@ -43,6 +45,16 @@ class Layout(ctypes.Structure):
     _fields_ = [
         ("dtype", c_int32), ("batch", c_int32), ("layers", c_int32), ("kv_heads", c_int32),
         ("capacity", c_int32), ("head_dim", c_int32),
+        ("stride_batch", c_int64), ("stride_layer", c_int64), ("stride_head", c_int64), ("stride_token", c_int64),
+    ]
+
+
+class Q8Layout(ctypes.Structure):
+    """Mirror of ``freqkv_q8_layout``."""
+
+    _fields_ = [
+        ("kind", c_int32), ("batch", c_int32), ("layers", c_int32), ("kv_heads", c_int32), ("capacity", c_int32),
+        ("head_dim", c_int32), ("block_tokens", c_int32),
         ("stride_batch", c_int64), ("stride_layer", c_int64), ("stride_head", c_int64), ("stride_token", c_int64),
     ]
 
@@ -103,6 +115,13 @@ def lib() -> ctypes.CDLL:
         L.freqkv_gemm_fold_levels.restype = c_int32
         L.freqkv_gemm_blocks.argtypes = [c_int32, c_int32, c_int32, c_int64]
         L.freqkv_gemm_blocks.restype = c_int32
+        QP = POINTER(Q8Layout)
+        four = [c_void_p] * 4   # codes of K and V, scales of K and V
+        L.freqkv_append_q8.argtypes = [c_void_p, QP, *four, c_void_p, c_void_p, c_int, c_int32, I32P, c_void_p]
+        L.freqkv_check_append_q8.argtypes = [QP, *four, c_void_p, c_void_p, c_int, c_int32, I32P]
+        L.freqkv_quantize.argtypes = [c_void_p, LP, c_void_p, c_void_p, I32P, QP, *four, c_void_p]
+        L.freqkv_dequantize.argtypes = [c_void_p, QP, *four, I32P, LP, c_void_p, c_void_p, c_void_p]
+        L.freqkv_check_quantize.argtypes = [LP, c_void_p, c_void_p, I32P, QP, *four]
         L.freqkv_last_error.argtypes = [c_void_p]
         L.freqkv_last_error.restype = c_char_p
         L.freqkv_status_string.argtypes = [c_int]
@@ -217,6 +236,40 @@ def compress_noalloc(k: torch.Tensor, v: torch.Tensor, cache_len: int, kept_len:
     if st != OK:
         raise FreqKVError(st, f"freqkv_compress_noalloc: {status_string(st)}")
     return sink + kept_len
+
+
+class Q8Cache:
+    """A cache in 8 bits: codes ``k``, ``v`` [batch, layers, kv_heads, capacity, head_dim] (``torch.int8`` or
+    ``torch.float8_e4m3fn``; a view with arbitrary strides is fine as long as head_dim is contiguous) and dense fp32 scales
+    ``k_scale``, ``v_scale`` [batch, layers, kv_heads, ceil(capacity / block_tokens)]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_tokens: int):
+        kinds = {torch.float8_e4m3fn: Q8_E4M3, torch.int8: Q8_INT8}
+        if k.dtype not in kinds:
+            raise FreqKVError(ERR_UNSUPPORTED, f"unsupported code type {k.dtype}")
+        if k.dim() != 5 or k.stride(4) != 1:
+            raise FreqKVError(ERR_UNSUPPORTED, "codes must be [batch, layers, kv_heads, capacity, head_dim] with contiguous head_dim")
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise FreqKVError(ERR_INVALID_ARG, "K and V must share shape, strides and dtype")
+        if block_tokens not in (16, 32, 64, 128):
+            raise FreqKVError(ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128")
+        want = (*k.shape[:3], -(-k.shape[3] // block_tokens))
+        for s in (k_scale, v_scale):
+            if s.dtype != torch.float32 or tuple(s.shape) != want or not s.is_contiguous() or s.device != k.device:
+                raise FreqKVError(ERR_INVALID_ARG, f"scales must be dense fp32 {want} on the codes' device")
+        self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
+        self.layout = Q8Layout(kinds[k.dtype], *k.shape, block_tokens, *k.stride()[:4])
+        self._ref = ctypes.byref(self.layout)
+        self._ptrs = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    @classmethod
+    def empty(cls, batch: int, layers: int, kv_heads: int, capacity: int, head_dim: int = 128, kind: int = Q8_E4M3,
+              block_tokens: int = 64, device="cuda") -> "Q8Cache":
+        """A dense cache without rows (codes and scales are zeros)."""
+        dtype = {Q8_E4M3: torch.float8_e4m3fn, Q8_INT8: torch.int8}[kind]
+        codes = [torch.zeros(batch, layers, kv_heads, capacity, head_dim, dtype=torch.int8, device=device).view(dtype) for _ in range(2)]
+        scales = [torch.zeros(batch, layers, kv_heads, -(-capacity // block_tokens), device=device) for _ in range(2)]
+        return cls(*codes, *scales, block_tokens)
 
 
 class DecodeGraph:
@@ -413,6 +466,42 @@ class Context:
                                          _stream_ptr(stream))
         self._check(st, "freqkv_attend_prefill")
         return out
+
+    def append_q8(self, cache: Q8Cache, new_k: torch.Tensor, new_v: torch.Tensor, lens: list[int], stream=None) -> list[int]:
+        """Append new_k / new_v ``[batch, layers, kv_heads, n_new, head_dim]`` (dense, bf16 or fp32) to an 8-bit cache; returns the
+        new lengths.  Raises FreqKVError(ERR_CAPACITY) when a sequence has no room."""
+        lay = cache.layout
+        if not (new_k.is_contiguous() and new_v.is_contiguous()) or new_k.shape != new_v.shape or new_k.dtype != new_v.dtype:
+            raise FreqKVError(ERR_INVALID_ARG, "new_k / new_v must be dense and of equal shape and dtype")
+        if new_k.dim() != 5 or new_k.shape[:3] != cache.k.shape[:3] or new_k.shape[4] != cache.k.shape[4] or len(lens) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "new rows or lens do not match the cache")
+        c_lens = (c_int32 * lay.batch)(*lens)
+        st = lib().freqkv_append_q8(self._h, cache._ref, *cache._ptrs, new_k.data_ptr(), new_v.data_ptr(), dtype_code(new_k.dtype),
+                                    new_k.shape[3], c_lens, _stream_ptr(stream))
+        self._check(st, "freqkv_append_q8")
+        return list(c_lens)
+
+    def quantize(self, k: torch.Tensor, v: torch.Tensor, lens: list[int], cache: Q8Cache, stream=None):
+        """Rows [0, lens[b]) of a bf16 or fp32 cache into an 8-bit one."""
+        lay = layout_of(k)
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise FreqKVError(ERR_INVALID_ARG, "K and V must share shape, strides and dtype")
+        if len(lens) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "lens needs one entry per sequence")
+        st = lib().freqkv_quantize(self._h, ctypes.byref(lay), k.data_ptr(), v.data_ptr(), (c_int32 * lay.batch)(*lens), cache._ref,
+                                   *cache._ptrs, _stream_ptr(stream))
+        self._check(st, "freqkv_quantize")
+
+    def dequantize(self, cache: Q8Cache, lens: list[int], k: torch.Tensor, v: torch.Tensor, stream=None):
+        """Rows [0, lens[b]) of a bf16 or fp32 cache <- those of an 8-bit one."""
+        lay = layout_of(k)
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise FreqKVError(ERR_INVALID_ARG, "K and V must share shape, strides and dtype")
+        if len(lens) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "lens needs one entry per sequence")
+        st = lib().freqkv_dequantize(self._h, cache._ref, *cache._ptrs, (c_int32 * lay.batch)(*lens), ctypes.byref(lay), k.data_ptr(),
+                                     v.data_ptr(), _stream_ptr(stream))
+        self._check(st, "freqkv_dequantize")
 
     def compress_host(self, k_host: torch.Tensor, v_host: torch.Tensor, cache_len: int, kept_len: int, sink: int,
                       stream=None) -> tuple[int, int, int]:

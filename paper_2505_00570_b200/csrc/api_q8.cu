@@ -1,0 +1,201 @@
+// C ABI of the cache in 8 bits: argument validation and dispatch.
+#include <algorithm>
+
+#include "ctx.cuh"
+#include "q8.cuh"
+
+using namespace freqkv;
+
+namespace {
+
+// The strides' rules are those of the other caches, for elements of one byte: rows of 16 bytes' multiples.
+freqkv_status check_q8_layout(const freqkv_q8_layout* l)
+{
+    if (!l) return FREQKV_ERR_INVALID_ARG;
+    if (l->kind != FREQKV_Q8_E4M3 && l->kind != FREQKV_Q8_INT8) return FREQKV_ERR_UNSUPPORTED;
+    const freqkv_layout as = {FREQKV_BF16,    l->batch,        l->layers,       l->kv_heads,    l->capacity,
+                              l->head_dim,    l->stride_batch, l->stride_layer, l->stride_head, l->stride_token};
+    const freqkv_status st = check_layout(&as);
+    if (st != FREQKV_OK) return st;
+    if (l->block_tokens != 16 && l->block_tokens != 32 && l->block_tokens != 64 && l->block_tokens != 128) return FREQKV_ERR_UNSUPPORTED;
+    if (l->head_dim % 16 != 0) return FREQKV_ERR_UNSUPPORTED;
+    const int64_t strides[4] = {l->stride_token, l->stride_head, l->stride_layer, l->stride_batch};
+    for (const int64_t s : strides)
+        if (s % 16 != 0) return FREQKV_ERR_UNSUPPORTED;
+    return FREQKV_OK;
+}
+
+bool apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
+{
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return x + a_bytes <= y || y + b_bytes <= x;
+}
+
+int64_t q8_span(const freqkv_q8_layout& l)
+{
+    return (int64_t)(l.batch - 1) * l.stride_batch + (int64_t)(l.layers - 1) * l.stride_layer + (int64_t)(l.kv_heads - 1) * l.stride_head +
+           (int64_t)(l.capacity - 1) * l.stride_token + l.head_dim;
+}
+
+int32_t q8_blocks(const freqkv_q8_layout& l) { return (l.capacity - 1) / l.block_tokens + 1; }
+
+// Layout and the four arrays: there, aligned, apart from one another.
+freqkv_status check_q8(const freqkv_q8_layout* l, const void* k, const void* v, const float* k_scale, const float* v_scale)
+{
+    const freqkv_status st = check_q8_layout(l);
+    if (st != FREQKV_OK) return st;
+    if (!k || !v || !k_scale || !v_scale) return FREQKV_ERR_INVALID_ARG;
+    if (((uintptr_t)k | (uintptr_t)v) & 15 || ((uintptr_t)k_scale | (uintptr_t)v_scale) & 3) return FREQKV_ERR_UNSUPPORTED;
+    const int64_t codes = q8_span(*l), scales = (int64_t)l->batch * l->layers * l->kv_heads * q8_blocks(*l) * 4;
+    const std::pair<const void*, int64_t> areas[4] = {{k, codes}, {v, codes}, {k_scale, scales}, {v_scale, scales}};
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < i; ++j)
+            if (!apart(areas[i].first, areas[i].second, areas[j].first, areas[j].second)) return FREQKV_ERR_INVALID_ARG;
+    return FREQKV_OK;
+}
+
+Q8View q8_view(const freqkv_q8_layout& l, const void* k, const void* v, const float* k_scale, const float* v_scale)
+{
+    Q8View w;
+    w.codes[0] = const_cast<void*>(k);
+    w.codes[1] = const_cast<void*>(v);
+    w.scales[0] = const_cast<float*>(k_scale);
+    w.scales[1] = const_cast<float*>(v_scale);
+    w.stride_batch = l.stride_batch;
+    w.stride_layer = l.stride_layer;
+    w.stride_head = l.stride_head;
+    w.stride_token = l.stride_token;
+    w.layers = l.layers;
+    w.kv_heads = l.kv_heads;
+    w.head_dim = l.head_dim;
+    w.blocks = q8_blocks(l);
+    w.block_tokens = l.block_tokens;
+    w.kind = l.kind;
+    return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+freqkv_status freqkv_check_append_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                     const float* v_scale, const void* new_k, const void* new_v, freqkv_dtype dtype, int32_t n_new,
+                                     const int32_t* lens)
+{
+    if (!lens) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = check_q8(layout, k, v, k_scale, v_scale);
+    if (st != FREQKV_OK) return st;
+    if (dtype != FREQKV_BF16 && dtype != FREQKV_F32) return FREQKV_ERR_UNSUPPORTED;
+    if (n_new < 0) return FREQKV_ERR_INVALID_ARG;
+    if (n_new > 0 && (!new_k || !new_v)) return FREQKV_ERR_INVALID_ARG;
+    if (n_new > 0 && (((uintptr_t)new_k | (uintptr_t)new_v) & 15)) return FREQKV_ERR_UNSUPPORTED;
+    for (int32_t b = 0; b < layout->batch; ++b) {
+        if (lens[b] < 0 || lens[b] > layout->capacity) return FREQKV_ERR_INVALID_ARG;
+        if ((int64_t)lens[b] + n_new > layout->capacity) return FREQKV_ERR_CAPACITY;
+    }
+    return FREQKV_OK;
+}
+
+freqkv_status freqkv_append_q8(freqkv_ctx* ctx, const freqkv_q8_layout* layout, void* k, void* v, float* k_scale, float* v_scale,
+                               const void* new_k, const void* new_v, freqkv_dtype dtype, int32_t n_new, int32_t* lens,
+                               void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_append_q8(layout, k, v, k_scale, v_scale, new_k, new_v, dtype, n_new, lens);
+    if (st != FREQKV_OK) return st;
+    if (n_new == 0) return FREQKV_OK;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    const freqkv_q8_layout& l = *layout;
+    Q8Source src;
+    src.rows[0] = new_k;
+    src.rows[1] = new_v;
+    src.dtype = dtype;
+    src.stride_token = l.head_dim;
+    src.stride_head = src.stride_token * n_new;
+    src.stride_layer = src.stride_head * l.kv_heads;
+    src.stride_batch = src.stride_layer * l.layers;
+    int32_t launched = 0;
+    const cudaError_t e = launch_quantize(q8_view(l, k, v, k_scale, v_scale), src, l.batch, lens, nullptr, n_new, &launched,
+                                          static_cast<cudaStream_t>(cuda_stream));
+    ctx->kernels_launched += launched;
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "append_q8");
+    for (int32_t b = 0; b < l.batch; ++b) lens[b] += n_new;
+    return FREQKV_OK;
+}
+
+freqkv_status freqkv_check_quantize(const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
+                                    const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                    const float* v_scale)
+{
+    if (!lens) return FREQKV_ERR_INVALID_ARG;
+    freqkv_status st = check_q8(layout, k, v, k_scale, v_scale);
+    if (st != FREQKV_OK) return st;
+    st = check_layout(src);
+    if (st != FREQKV_OK) return st;
+    st = check_tensors(*src, k_src, v_src);
+    if (st != FREQKV_OK) return st;
+    if (src->batch != layout->batch || src->layers != layout->layers || src->kv_heads != layout->kv_heads || src->head_dim != layout->head_dim)
+        return FREQKV_ERR_INVALID_ARG;
+    const int64_t rows = span_elements(*src) * (int64_t)dtype_size(src->dtype), codes = q8_span(*layout),
+                  scales = (int64_t)layout->batch * layout->layers * layout->kv_heads * q8_blocks(*layout) * 4;
+    for (const void* x : {k_src, v_src})
+        if (!apart(x, rows, k, codes) || !apart(x, rows, v, codes) || !apart(x, rows, k_scale, scales) || !apart(x, rows, v_scale, scales))
+            return FREQKV_ERR_INVALID_ARG;
+    for (int32_t b = 0; b < layout->batch; ++b)
+        if (lens[b] < 0 || lens[b] > layout->capacity || lens[b] > src->capacity) return FREQKV_ERR_INVALID_ARG;
+    return FREQKV_OK;
+}
+
+freqkv_status freqkv_quantize(freqkv_ctx* ctx, const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
+                              const freqkv_q8_layout* layout, void* k, void* v, float* k_scale, float* v_scale, void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_quantize(src, k_src, v_src, lens, layout, k, v, k_scale, v_scale);
+    if (st != FREQKV_OK) return st;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    Q8Source from;
+    from.rows[0] = k_src;
+    from.rows[1] = v_src;
+    from.dtype = src->dtype;
+    from.stride_batch = src->stride_batch;
+    from.stride_layer = src->stride_layer;
+    from.stride_head = src->stride_head;
+    from.stride_token = src->stride_token;
+    int32_t launched = 0;
+    const cudaError_t e = launch_quantize(q8_view(*layout, k, v, k_scale, v_scale), from, layout->batch, nullptr, lens, 0, &launched,
+                                          static_cast<cudaStream_t>(cuda_stream));
+    ctx->kernels_launched += launched;
+    return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "quantize");
+}
+
+freqkv_status freqkv_dequantize(freqkv_ctx* ctx, const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                const float* v_scale, const int32_t* lens, const freqkv_layout* dst, void* k_dst, void* v_dst,
+                                void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_quantize(dst, k_dst, v_dst, lens, layout, k, v, k_scale, v_scale);
+    if (st != FREQKV_OK) return st;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    CacheView out;
+    out.base[0] = k_dst;
+    out.base[1] = v_dst;
+    out.stride_batch = dst->stride_batch;
+    out.stride_layer = dst->stride_layer;
+    out.stride_head = dst->stride_head;
+    out.stride_token = dst->stride_token;
+    out.layers = dst->layers;
+    out.kv_heads = dst->kv_heads;
+    out.head_dim = dst->head_dim;
+    out.mats_per_tensor = dst->batch * dst->layers * dst->kv_heads;
+    out.batch0 = 0;
+    int32_t launched = 0;
+    const cudaError_t e = launch_dequantize(q8_view(*layout, k, v, k_scale, v_scale), out, dst->dtype, layout->batch, lens, &launched,
+                                            static_cast<cudaStream_t>(cuda_stream));
+    ctx->kernels_launched += launched;
+    return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "dequantize");
+}
+
+}  // extern "C"

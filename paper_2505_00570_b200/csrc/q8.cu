@@ -1,0 +1,387 @@
+// Rows into the cache in 8 bits, and out of it.
+//
+// Every (batch, layer, kv_head) matrix of K and of V is cut into blocks of `block_tokens` rows, each with one fp32 scale s; a
+// value is code * s.  With a the largest finite magnitude of the rows that enter a block:
+//   INT8  s = a / 127 rounded to fp32 (at least 2^-126), code = x / s rounded to the nearest integer, ties to even;
+//   E4M3  s = the smallest power of two with a <= 448 s (at least 2^-126), code = x / s rounded to e4m3, ties to even.
+// A power of two for E4M3: a floating code has the same relative step under any scale, x / s is exact, and a scale that grows
+// moves old codes without rounding them (but for those that become subnormal).
+// Rows that enter a block which has rows already leave the scale alone if they fit, else it grows and the old codes are
+// rounded again: code * s_old / s.
+//
+// Bound by memory: 2 (or 4) bytes read and 1 written a value.  A block's values stay in registers between the look for their
+// largest magnitude and their rounding, so they are read once: 8 values a chunk, as many chunks a lane as the block's warps (one
+// for every 16 rows) need.  The quotient is taken as a product with 1 / s and looked at again only where it falls within 2^-10
+// of a tie (the product is off by at most 127 * 2^-23): there the remainder, exact in one fma, decides.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "q8.cuh"
+
+namespace freqkv {
+namespace {
+
+constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr float TINY = 1.17549435e-38f;  // 2^-126: no scale is subnormal, so that 1 / s is finite
+constexpr float INF = __builtin_huge_valf();
+
+struct WriteParams {
+    Q8View cache;
+    Q8Source src;
+    int32_t batch0, groups;           // CTAs a matrix
+    int32_t begin[Q8_MAX_BATCH], end[Q8_MAX_BATCH];
+};
+
+// 8 consecutive values as loaded.
+template <typename T>
+struct Chunk;
+template <>
+struct Chunk<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { u = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void clear() { u = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    // Largest magnitude, NaN if one of the values is NaN.
+    __device__ __forceinline__ float largest() const
+    {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[0]));
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[i])));
+        const float2 f = __bfloat1622float2(m);
+        return f.x != f.x || f.y != f.y ? f.x + f.y : fmaxf(f.x, f.y);
+    }
+};
+template <>
+struct Chunk<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p)
+    {
+        a = __ldcs(reinterpret_cast<const float4*>(p));
+        b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+    __device__ __forceinline__ float largest() const
+    {
+        float x[8], m = 0.f, nan = 0.f;
+        get(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            m = fmaxf(m, fabsf(x[i]));
+            nan += x[i] * 0.f;  // NaN for infinities, too: those blocks take the careful way as well
+        }
+        return nan != nan ? nan : m;
+    }
+};
+
+__device__ __forceinline__ float scale_of(float largest, int32_t kind)
+{
+    if (!(largest > 0.f)) return 0.f;
+    if (kind == FREQKV_Q8_INT8) return fmaxf(__fdiv_rn(largest, 127.f), TINY);
+    // largest = m 2^e with m in [1, 2), 448 = 1.75 * 2^8: s = 2^(e - 8), one more where m > 1.75
+    const uint32_t bits = __float_as_uint(largest);
+    const int32_t e = (int32_t)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u);  // biased exponent of s (subnormals: below 1)
+    return __uint_as_float((uint32_t)max(e, 1) << 23);
+}
+
+// The integer nearest to the quotient x / s, ties to even; inv = 1 / s rounded.  |x| <= 127 s (1 + 2^-22), finite.
+__device__ __forceinline__ float nearest(float x, float s, float inv)
+{
+    const float t = x * inv;
+    float r = rintf(t);
+    if (fabsf(t - r) > 0.4990234375f) {
+        const float rest = fmaf(-r, s, x), off = fabsf(rest) - (s - fabsf(rest));  // both exact: rest is at most s, a multiple of the smaller last place
+        if (off > 0.f || (off == 0.f && ((int)r & 1))) r += rest > 0.f ? 1.f : -1.f;
+    }
+    return r;
+}
+
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d)
+{
+    const uint32_t lo = __byte_perm((uint32_t)(int)a, (uint32_t)(int)b, 0x0040), hi = __byte_perm((uint32_t)(int)c, (uint32_t)(int)d, 0x0040);
+    return __byte_perm(lo, hi, 0x5410);
+}
+__device__ __forceinline__ uint32_t e4m3x2(float a, float b)
+{
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+
+template <int KIND>
+__device__ __forceinline__ uint2 codes_of(float (&x)[8], float s, float inv, bool special)
+{
+    if constexpr (KIND == FREQKV_Q8_INT8) {
+        if (special) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -127.f * s), 127.f * s) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(nearest(x[i], s, inv), -127.f), 127.f);
+        return make_uint2(pack4(x[0], x[1], x[2], x[3]), pack4(x[4], x[5], x[6], x[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= inv;  // a power of two: exact (what falls below fp32's range rounds to zero in e4m3, too)
+        return make_uint2(e4m3x2(x[0], x[1]) | e4m3x2(x[2], x[3]) << 16, e4m3x2(x[4], x[5]) | e4m3x2(x[6], x[7]) << 16);
+    }
+}
+
+// An old code under a scale that has grown from s_old to s.
+template <int KIND>
+__device__ __forceinline__ uint8_t again(uint8_t code, float s_old, float s)
+{
+    if constexpr (KIND == FREQKV_Q8_INT8) {
+        // 64 bits: the product is exact and a quotient that is not a tie stays clear of one
+        return (uint8_t)(int8_t)(int)rint((double)(int8_t)code * (double)s_old / (double)s);
+    } else {
+        const __half_raw h = __nv_cvt_fp8_to_halfraw(code, __NV_E4M3);
+        return __nv_cvt_float_to_fp8(__half2float(__half(h)) * (s_old / s), __NV_SATFINITE, __NV_E4M3);
+    }
+}
+
+// A CTA takes 8 / WPB blocks of one matrix, WPB = block_tokens / 16 warps each.  NCH: chunks a lane holds.
+template <typename T, int KIND, int NCH, bool D128>
+__global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant__ WriteParams p)
+{
+    __shared__ float sm_max[WARPS];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int32_t bt = p.cache.block_tokens, wpb = bt / 16, per_cta = WARPS / wpb;
+    // matrix and first block
+    const int32_t group = (int32_t)(blockIdx.x % (uint32_t)p.groups);
+    int32_t mat = (int32_t)(blockIdx.x / (uint32_t)p.groups);
+    const int tensor = mat & 1;
+    mat >>= 1;
+    const int32_t h = mat % p.cache.kv_heads, lb = mat / p.cache.kv_heads, l = lb % p.cache.layers, b = lb / p.cache.layers;
+    const int32_t begin = p.begin[b], end = p.end[b];
+    const int32_t block = begin / bt + group * per_cta + warp / wpb, at = block * bt;
+    const int32_t lo = max(begin, at), hi = min(end, at + bt);  // new rows of this block (none: lo >= hi)
+    const int32_t chunks_row = D128 ? 16 : p.cache.head_dim / 8;
+    const int32_t n_chunks = (hi - lo) * chunks_row;
+    const int64_t bb = p.batch0 + b;
+    const T* src = static_cast<const T*>(p.src.rows[tensor]) + bb * p.src.stride_batch + l * p.src.stride_layer + h * p.src.stride_head +
+                   (int64_t)(lo - begin) * p.src.stride_token;
+    uint8_t* dst = static_cast<uint8_t*>(p.cache.codes[tensor]) + bb * p.cache.stride_batch + l * p.cache.stride_layer + h * p.cache.stride_head;
+    float* scale = p.cache.scales[tensor] + ((bb * p.cache.layers + l) * p.cache.kv_heads + h) * p.cache.blocks + block;
+
+    const int32_t first = (warp % wpb) * 32 + lane, step = wpb * 32;
+    const float s_old = lo < hi && lo > at ? *scale : 0.f;  // rows that are there already
+    Chunk<T> v[NCH];
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+        const int32_t ch = first + i * step;
+        if (ch < n_chunks) {
+            const int32_t row = D128 ? ch >> 4 : ch / chunks_row, c = (D128 ? ch & 15 : ch - row * chunks_row) * 8;
+            v[i].load(src + (int64_t)row * p.src.stride_token + c);
+        } else {
+            v[i].clear();
+        }
+    }
+    bool special = false;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+        const float f = v[i].largest();
+        special |= !(f < INF);
+        m = fmaxf(m, f);
+    }
+    special = __any_sync(0xffffffffu, special);
+    if (special) {  // infinities or NaN among them: the largest finite magnitude, value by value
+        m = 0.f;
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            float x[8];
+            v[i].get(x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (fabsf(x[j]) < INF) m = fmaxf(m, fabsf(x[j]));
+        }
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    if (wpb > 1) {
+        if (lane == 0) sm_max[warp] = m;
+        __syncthreads();  // s_old has been read by every warp of the block, too
+        for (int w = warp / wpb * wpb; w < warp / wpb * wpb + wpb; ++w) m = fmaxf(m, sm_max[w]);
+    } else {
+        __syncwarp();
+    }
+    if (lo >= hi) return;
+    const float s = fmaxf(s_old, scale_of(m, KIND)), inv = s > 0.f ? 1.f / s : 0.f;
+    if (lane == 0 && warp % wpb == 0) *scale = s;
+    const uint2 none = make_uint2(0u, 0u);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+        const int32_t ch = first + i * step;
+        if (ch < n_chunks) {
+            const int32_t row = D128 ? ch >> 4 : ch / chunks_row, c = (D128 ? ch & 15 : ch - row * chunks_row) * 8;
+            float x[8];
+            v[i].get(x);
+            *reinterpret_cast<uint2*>(dst + (int64_t)(lo + row) * p.cache.stride_token + c) =
+                s > 0.f || special ? codes_of<KIND>(x, s > 0.f ? s : 1.f, s > 0.f ? inv : 1.f, special) : none;
+        }
+    }
+    if (lo > at && s > s_old) {  // the scale has grown: the old rows of the block again
+        const int32_t old = (lo - at) * chunks_row;
+        for (int32_t ch = first; ch < old; ch += step) {
+            const int32_t row = D128 ? ch >> 4 : ch / chunks_row, c = (D128 ? ch & 15 : ch - row * chunks_row) * 8;
+            uint2* q = reinterpret_cast<uint2*>(dst + (int64_t)(at + row) * p.cache.stride_token + c);
+            uint2 u = *q;
+            uint32_t w[2] = {u.x, u.y};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                uint32_t r = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r |= (uint32_t)again<KIND>((uint8_t)(w[k] >> (8 * j)), s_old, s) << (8 * j);
+                w[k] = r;
+            }
+            *q = make_uint2(w[0], w[1]);
+        }
+    }
+}
+
+struct ReadParams {
+    Q8View cache;
+    CacheView out;
+    int32_t batch0, groups;  // CTAs a matrix
+    int32_t len[Q8_MAX_BATCH];
+};
+
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8])
+{
+    uint4 u;
+    __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(&u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    *reinterpret_cast<uint4*>(p) = u;
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8])
+{
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+constexpr int READ_CHUNKS = 4;  // of 8 codes a thread
+
+template <typename T, int KIND>
+__global__ void __launch_bounds__(THREADS) dequantize_kernel(const __grid_constant__ ReadParams p)
+{
+    const int32_t group = (int32_t)(blockIdx.x % (uint32_t)p.groups);
+    int32_t mat = (int32_t)(blockIdx.x / (uint32_t)p.groups);
+    const int tensor = mat & 1;
+    mat >>= 1;
+    const int32_t h = mat % p.cache.kv_heads, lb = mat / p.cache.kv_heads, l = lb % p.cache.layers, b = lb / p.cache.layers;
+    const int64_t bb = p.batch0 + b;
+    const int32_t chunks_row = p.cache.head_dim / 8;
+    const int64_t n = (int64_t)p.len[b] * chunks_row;
+    const uint8_t* src = static_cast<const uint8_t*>(p.cache.codes[tensor]) + bb * p.cache.stride_batch + l * p.cache.stride_layer + h * p.cache.stride_head;
+    T* dst = static_cast<T*>(tensor_base(p.out, tensor)) + bb * p.out.stride_batch + l * p.out.stride_layer + h * p.out.stride_head;
+    const float* scale = p.cache.scales[tensor] + ((bb * p.cache.layers + l) * p.cache.kv_heads + h) * p.cache.blocks;
+    const int64_t ch0 = (int64_t)group * (THREADS * READ_CHUNKS) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < READ_CHUNKS; ++i) {
+        const int64_t ch = ch0 + i * THREADS;
+        if (ch >= n) break;
+        const int32_t row = (int32_t)(ch / chunks_row), c = (int32_t)(ch - (int64_t)row * chunks_row) * 8;
+        const uint2 u = *reinterpret_cast<const uint2*>(src + (int64_t)row * p.cache.stride_token + c);
+        const float s = scale[row / p.cache.block_tokens];
+        const uint32_t w[2] = {u.x, u.y};
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint8_t code = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+            x[j] = s * (KIND == FREQKV_Q8_INT8 ? (float)(int8_t)code : __half2float(__half(__nv_cvt_fp8_to_halfraw(code, __NV_E4M3))));
+        }
+        store8(dst + (int64_t)row * p.out.stride_token + c, x);
+    }
+}
+
+template <typename T, int KIND>
+void launch_typed(const WriteParams& prm, uint32_t grid, cudaStream_t stream)
+{
+    if (prm.cache.head_dim == 128)
+        quantize_kernel<T, KIND, 8, true><<<grid, THREADS, 0, stream>>>(prm);
+    else if (prm.cache.head_dim <= 128)
+        quantize_kernel<T, KIND, 8, false><<<grid, THREADS, 0, stream>>>(prm);
+    else
+        quantize_kernel<T, KIND, 16, false><<<grid, THREADS, 0, stream>>>(prm);
+}
+
+}  // namespace
+
+cudaError_t launch_quantize(const Q8View& cache, const Q8Source& src, int32_t batch, const int32_t* begin, const int32_t* count,
+                            int32_t n_new, int32_t* launched, cudaStream_t stream)
+{
+    *launched = 0;
+    WriteParams prm;
+    prm.cache = cache;
+    prm.src = src;
+    const int32_t per_cta = WARPS / (cache.block_tokens / 16);
+    for (int32_t b0 = 0; b0 < batch; b0 += Q8_MAX_BATCH) {
+        const int32_t nb = std::min(Q8_MAX_BATCH, batch - b0);
+        int32_t most = 0;  // blocks that a sequence's rows touch
+        for (int32_t i = 0; i < nb; ++i) {
+            prm.begin[i] = begin ? begin[b0 + i] : 0;
+            prm.end[i] = prm.begin[i] + (count ? count[b0 + i] : n_new);
+            if (prm.end[i] > prm.begin[i]) most = std::max(most, (prm.end[i] - 1) / cache.block_tokens - prm.begin[i] / cache.block_tokens + 1);
+        }
+        if (most == 0) continue;
+        prm.batch0 = b0;
+        prm.groups = (most + per_cta - 1) / per_cta;
+        const int64_t grid = (int64_t)2 * nb * cache.layers * cache.kv_heads * prm.groups;
+        if (grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        const bool f32 = src.dtype == FREQKV_F32;
+        if (cache.kind == FREQKV_Q8_INT8)
+            f32 ? launch_typed<float, FREQKV_Q8_INT8>(prm, (uint32_t)grid, stream) : launch_typed<__nv_bfloat16, FREQKV_Q8_INT8>(prm, (uint32_t)grid, stream);
+        else
+            f32 ? launch_typed<float, FREQKV_Q8_E4M3>(prm, (uint32_t)grid, stream) : launch_typed<__nv_bfloat16, FREQKV_Q8_E4M3>(prm, (uint32_t)grid, stream);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launched;
+    }
+    return cudaSuccess;
+}
+
+cudaError_t launch_dequantize(const Q8View& cache, const CacheView& out, int32_t dtype, int32_t batch, const int32_t* lens,
+                              int32_t* launched, cudaStream_t stream)
+{
+    *launched = 0;
+    ReadParams prm;
+    prm.cache = cache;
+    prm.out = out;
+    for (int32_t b0 = 0; b0 < batch; b0 += Q8_MAX_BATCH) {
+        const int32_t nb = std::min(Q8_MAX_BATCH, batch - b0);
+        int64_t most = 0;
+        for (int32_t i = 0; i < nb; ++i) {
+            prm.len[i] = lens[b0 + i];
+            most = std::max(most, (int64_t)lens[b0 + i] * (cache.head_dim / 8));
+        }
+        if (most == 0) continue;
+        prm.batch0 = b0;
+        prm.groups = (int32_t)((most + THREADS * READ_CHUNKS - 1) / (THREADS * READ_CHUNKS));
+        const int64_t grid = (int64_t)2 * nb * cache.layers * cache.kv_heads * prm.groups;
+        if (grid > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        auto launch = [&](auto* kernel) { kernel<<<(uint32_t)grid, THREADS, 0, stream>>>(prm); };
+        if (cache.kind == FREQKV_Q8_INT8)
+            dtype == FREQKV_F32 ? launch(dequantize_kernel<float, FREQKV_Q8_INT8>) : launch(dequantize_kernel<__nv_bfloat16, FREQKV_Q8_INT8>);
+        else
+            dtype == FREQKV_F32 ? launch(dequantize_kernel<float, FREQKV_Q8_E4M3>) : launch(dequantize_kernel<__nv_bfloat16, FREQKV_Q8_E4M3>);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launched;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace freqkv
