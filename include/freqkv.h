@@ -327,6 +327,17 @@ freqkv_status freqkv_dequantize(freqkv_ctx* ctx, const freqkv_q8_layout* layout,
                                 const float* v_scale, const int32_t* lens, const freqkv_layout* dst, void* k_dst, void* v_dst,
                                 void* cuda_stream);
 
+/* freqkv_attend_decode over an 8-bit cache: the same attention, positions and layout of q and out (bf16, dense [batch, kv_heads *
+ * q_heads_per_kv, head_dim]), with keys and values  code * scale.  Any q_heads_per_kv from 1 to 64 (above 8 they are taken in groups of
+ * 8, each of which reads the cache).  Turned keys (as multiples of their block's scale), scaled queries and softmax weights are
+ * rounded to fp16, sums are fp32, the result is rounded once to bf16;  1.5 * scale * log2(e) * q  must stay below 65504 in magnitude.
+ * Capture, work areas and the order with following launches as for freqkv_attend_decode.  Errors: INVALID_ARG (null pointers, q == out, layer out of
+ * range, q_heads_per_kv < 1, a length outside [1, capacity], NaN scale or base), UNSUPPORTED (head_dim != 128, q_heads_per_kv > 64,
+ * misaligned pointers, the rules of freqkv_q8_layout), ALLOC, CUDA. */
+freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                      const float* v_scale, int32_t layer, const void* q, void* out, int32_t q_heads_per_kv,
+                                      const int32_t* lens, float rope_base, float scale, void* cuda_stream);
+
 /* Instrumentation for benchmarks.  With timing enabled every compression records a CUDA event
  * pair on the caller's stream around its transform kernel (the projection / fast-transform
  * launch, not the copy-back or table builders; the folded fp32 product's three launches together).  freqkv_get_timing waits for the recorded
@@ -404,6 +415,9 @@ freqkv_status freqkv_check_attend_prefill(const freqkv_layout* layout, const voi
 
 freqkv_status freqkv_check_append_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
                                      const float* v_scale, const void* new_k, const void* new_v, freqkv_dtype dtype, int32_t n_new,
+                                     const int32_t* lens);
+freqkv_status freqkv_check_attend_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                     const float* v_scale, int32_t layer, const void* q, const void* out, int32_t q_heads_per_kv,
                                      const int32_t* lens);
 /* (of freqkv_quantize and freqkv_dequantize alike) */
 freqkv_status freqkv_check_quantize(const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,

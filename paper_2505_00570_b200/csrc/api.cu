@@ -27,6 +27,8 @@ using namespace freqkv;
 // ---- what ctx.cuh declares ----
 namespace freqkv {
 
+constexpr size_t kAttendWorkBytes = size_t(16) << 20;   // decode attention: a work area that grows, grows ahead of need up to this
+
 freqkv_status cuda_fail(freqkv_ctx* ctx, cudaError_t e, const char* where)
 {
     if (ctx) ctx->last_error = std::string(where) + ": " + cudaGetErrorString(e);
@@ -44,13 +46,14 @@ bool is_capturing(cudaStream_t stream)
     return status != cudaStreamCaptureStatusNone;
 }
 
-WorkOrder::WorkOrder(freqkv_ctx* c, cudaStream_t s) : ctx(c), stream(s)
+WorkOrder::WorkOrder(freqkv_ctx* c, cudaStream_t s) : ctx(c), stream(s), captured(is_capturing(s))
 {
-    if (ctx->work_recorded && ctx->work_stream != stream) cudaStreamWaitEvent(stream, ctx->work_done, 0);
+    if (!captured && ctx->work_recorded && ctx->work_stream != stream) cudaStreamWaitEvent(stream, ctx->work_done, 0);
 }
 
 WorkOrder::~WorkOrder()
 {
+    if (captured) return;
     if (!ctx->work_done && cudaEventCreateWithFlags(&ctx->work_done, cudaEventDisableTiming) != cudaSuccess) {
         ctx->work_done = nullptr;
         cudaGetLastError();
@@ -134,6 +137,59 @@ freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base,
     return FREQKV_OK;
 }
 
+// The layers of a step are attended with the same lengths: the split of their rows (up to 18 candidates x batch divisions, 35 us
+// for a batch of 1000) is worked out once for equal values of everything it follows from.
+AttendPlan attend_plan_for(freqkv_ctx* ctx, int32_t batch, int32_t groups, int64_t resident, const int32_t* lens)
+{
+    const int32_t key[3] = {batch, groups, (int32_t)resident};
+    const size_t bytes = (size_t)batch * sizeof(int32_t);
+    if (std::memcmp(key, ctx->attend_key, sizeof(key)) == 0 && std::memcmp(lens, ctx->attend_lens, bytes) == 0) return ctx->attend_last;
+    const AttendPlan plan = attend_plan(batch, lens, groups, resident);
+    if (batch > ctx->attend_lens_room) {
+        std::free(ctx->attend_lens);
+        ctx->attend_lens = static_cast<int32_t*>(std::malloc(bytes));
+        ctx->attend_lens_room = ctx->attend_lens ? batch : 0;
+    }
+    if (ctx->attend_lens) {
+        std::memcpy(ctx->attend_lens, lens, bytes);
+        std::memcpy(ctx->attend_key, key, sizeof(key));
+        ctx->attend_last = plan;
+    } else {
+        ctx->attend_key[0] = 0;  // no batch has this size
+    }
+    return plan;
+}
+
+freqkv_status attend_work_for(freqkv_ctx* ctx, const AttendPlan& plan, int32_t batch, int32_t q_heads, int32_t capacity, size_t more,
+                              cudaStream_t stream, AttendWork* out)
+{
+    const size_t tickets = attend_ticket_bytes(ctx->sm_count), partial = (attend_partial_bytes(plan.splits, batch, q_heads) + 255) & ~(size_t)255;
+    const size_t need = tickets + partial + more;
+    if (need > ctx->attend_work_bytes) {
+        size_t bytes = need;
+        if (ctx->attend_work) {
+            // The batch or its lengths have grown: room for the most splits that this batch can have, so that a stream of calls
+            // stops here once.  (Not at the first call: allocating 6 instead of 1 MB makes it 0.3 ms longer.)
+            const size_t most = tickets + attend_partial_bytes(attend_most_splits(capacity), batch, q_heads);
+            bytes = std::max(need, std::min(most, kAttendWorkBytes) + more);
+            FREQKV_CUDA(ctx, cudaDeviceSynchronize());
+            cudaFree(ctx->attend_work);
+            ctx->attend_work = nullptr;
+            ctx->attend_work_bytes = 0;
+        }
+        ctx->attend_tickets_clear = false;
+        FREQKV_CUDA(ctx, cudaMalloc(&ctx->attend_work, bytes));
+        ctx->attend_work_bytes = bytes;
+    }
+    if (plan.one_wave && !plan.captured && !ctx->attend_tickets_clear) {
+        FREQKV_CUDA(ctx, cudaMemsetAsync(ctx->attend_work, 0, tickets, stream));
+        ctx->attend_tickets_clear = true;
+    }
+    char* base = static_cast<char*>(ctx->attend_work);
+    *out = {reinterpret_cast<int32_t*>(base), reinterpret_cast<float*>(base + tickets), base + tickets + partial};
+    return FREQKV_OK;
+}
+
 }  // namespace freqkv
 
 namespace {
@@ -141,7 +197,6 @@ namespace {
 constexpr size_t kScratchChunkBytes = size_t(1) << 30;  // per-chunk output staging of the scratch paths
 constexpr int32_t kDctRows = -1;  // plan key of the plain DCT matrix (power spectrum) among the retained-band offsets
 constexpr size_t kBasisBudgetBytes = size_t(12) << 30;  // plan cache is flushed beyond this
-constexpr size_t kAttendWorkBytes = size_t(16) << 20;   // decode attention: a work area that grows, grows ahead of need up to this
 
 CacheView make_view(const freqkv_layout& l, void* k, void* v, int32_t batch0, int32_t batch_count)
 {
@@ -1054,29 +1109,6 @@ freqkv_status freqkv_check_attend(const freqkv_layout* layout, const void* k, co
     return FREQKV_OK;
 }
 
-// The layers of a step are attended with the same lengths: the split of their rows (up to 18 candidates x batch divisions, 35 us
-// for a batch of 1000) is worked out once for equal values of everything it follows from.
-static AttendPlan attend_plan_for(freqkv_ctx* ctx, const freqkv_layout& l, int32_t q_heads_per_kv, const int32_t* lens)
-{
-    const int32_t key[4] = {l.batch, l.kv_heads, q_heads_per_kv, l.dtype};
-    const size_t bytes = (size_t)l.batch * sizeof(int32_t);
-    if (std::memcmp(key, ctx->attend_key, sizeof(key)) == 0 && std::memcmp(lens, ctx->attend_lens, bytes) == 0) return ctx->attend_last;
-    const AttendPlan plan = attend_plan(l.batch, lens, l.kv_heads, q_heads_per_kv, l.dtype, ctx->sm_count);
-    if (l.batch > ctx->attend_lens_room) {
-        std::free(ctx->attend_lens);
-        ctx->attend_lens = static_cast<int32_t*>(std::malloc(bytes));
-        ctx->attend_lens_room = ctx->attend_lens ? l.batch : 0;
-    }
-    if (ctx->attend_lens) {
-        std::memcpy(ctx->attend_lens, lens, bytes);
-        std::memcpy(ctx->attend_key, key, sizeof(key));
-        ctx->attend_last = plan;
-    } else {
-        ctx->attend_key[0] = 0;  // no batch has this size
-    }
-    return plan;
-}
-
 freqkv_status freqkv_attend_decode(freqkv_ctx* ctx, const freqkv_layout* layout, const void* k, const void* v, int32_t layer,
                                    const void* q, void* out, int32_t q_heads_per_kv, const int32_t* lens, float rope_base,
                                    float scale, void* cuda_stream)
@@ -1094,39 +1126,17 @@ freqkv_status freqkv_attend_decode(freqkv_ctx* ctx, const freqkv_layout* layout,
     const float2* table = nullptr;
     const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
-    AttendPlan plan = attend_plan_for(ctx, l, q_heads_per_kv, lens);
-    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-    FREQKV_CUDA(ctx, cudaStreamIsCapturing(stream, &capture));
-    plan.captured = capture != cudaStreamCaptureStatusNone;
-    const size_t tickets = attend_ticket_bytes(ctx->sm_count);
-    const size_t need = tickets + attend_partial_bytes(plan.splits, l.batch, l.kv_heads * q_heads_per_kv);
-    if (need > ctx->attend_work_bytes) {
-        size_t bytes = need;
-        if (ctx->attend_work) {
-            // The batch or its lengths have grown: room for the most splits that this batch can have, so that a stream of calls
-            // stops here once.  (Not at the first call: allocating 6 instead of 1 MB makes it 0.3 ms longer.)
-            const size_t most = tickets + attend_partial_bytes(attend_most_splits(l.capacity), l.batch, l.kv_heads * q_heads_per_kv);
-            bytes = std::max(need, std::min(most, kAttendWorkBytes));
-            FREQKV_CUDA(ctx, cudaDeviceSynchronize());
-            cudaFree(ctx->attend_work);
-            ctx->attend_work = nullptr;
-            ctx->attend_work_bytes = 0;
-        }
-        ctx->attend_tickets_clear = false;
-        FREQKV_CUDA(ctx, cudaMalloc(&ctx->attend_work, bytes));
-        ctx->attend_work_bytes = bytes;
-    }
-    if (plan.one_wave && !plan.captured && !ctx->attend_tickets_clear) {
-        FREQKV_CUDA(ctx, cudaMemsetAsync(ctx->attend_work, 0, tickets, stream));
-        ctx->attend_tickets_clear = true;
-    }
+    AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads, attend_resident(q_heads_per_kv, l.dtype, ctx->sm_count), lens);
+    plan.captured = is_capturing(stream);
+    AttendWork work;
+    const freqkv_status ws = attend_work_for(ctx, plan, l.batch, l.kv_heads * q_heads_per_kv, l.capacity, 0, stream, &work);
+    if (ws != FREQKV_OK) return ws;
     int32_t launched = 0;
     cudaError_t e;
     {
         TransformTimer timer(ctx, stream);
-        e = launch_attend(l, k, v, layer, q, out, q_heads_per_kv, lens, table, scale, plan,
-                          reinterpret_cast<float*>(static_cast<char*>(ctx->attend_work) + tickets),
-                          static_cast<int32_t*>(ctx->attend_work), &launched, stream);
+        e = launch_attend(l, k, v, layer, q, out, q_heads_per_kv, lens, table, scale, plan, work.partial,
+                          work.tickets, &launched, stream);
     }
     ctx->kernels_launched += launched;
     if (e != cudaSuccess) return cuda_fail(ctx, e, "attend");

@@ -1,7 +1,9 @@
 // C ABI of the cache in 8 bits: argument validation and dispatch.
 #include <algorithm>
+#include <cmath>
 
 #include "ctx.cuh"
+#include "attend_q8.cuh"
 #include "q8.cuh"
 
 using namespace freqkv;
@@ -196,6 +198,55 @@ freqkv_status freqkv_dequantize(freqkv_ctx* ctx, const freqkv_q8_layout* layout,
                                             static_cast<cudaStream_t>(cuda_stream));
     ctx->kernels_launched += launched;
     return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "dequantize");
+}
+
+freqkv_status freqkv_check_attend_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                     const float* v_scale, int32_t layer, const void* q, const void* out, int32_t q_heads_per_kv,
+                                     const int32_t* lens)
+{
+    if (!lens) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = check_q8(layout, k, v, k_scale, v_scale);
+    if (st != FREQKV_OK) return st;
+    if (!q || !out || q == out) return FREQKV_ERR_INVALID_ARG;
+    if (((uintptr_t)q | (uintptr_t)out) & 15) return FREQKV_ERR_UNSUPPORTED;
+    if (layer < 0 || layer >= layout->layers || q_heads_per_kv < 1) return FREQKV_ERR_INVALID_ARG;
+    if (layout->head_dim != 128 || q_heads_per_kv > 64 || (int64_t)layout->kv_heads * q_heads_per_kv > 65535) return FREQKV_ERR_UNSUPPORTED;
+    for (int32_t b = 0; b < layout->batch; ++b)
+        if (lens[b] < 1 || lens[b] > layout->capacity) return FREQKV_ERR_INVALID_ARG;
+    return FREQKV_OK;
+}
+
+freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                      const float* v_scale, int32_t layer, const void* q, void* out, int32_t q_heads_per_kv,
+                                      const int32_t* lens, float rope_base, float scale, void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_attend_q8(layout, k, v, k_scale, v_scale, layer, q, out, q_heads_per_kv, lens);
+    if (st != FREQKV_OK) return st;
+    if (!(scale == scale) || !(rope_base == rope_base)) return FREQKV_ERR_INVALID_ARG;  // NaN
+    const freqkv_q8_layout& l = *layout;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    WorkOrder order(ctx, stream);
+    if (scale <= 0.f) scale = 1.0f / sqrtf((float)l.head_dim);
+    const float2* table = nullptr;
+    const freqkv_status ts = rope_table_for(ctx, std::max(l.capacity, 16), rope_base, stream, &table);
+    if (ts != FREQKV_OK) return ts;
+    AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads * q8_head_groups(q_heads_per_kv), attend_q8_resident(ctx->sm_count), lens);
+    plan.captured = is_capturing(stream);
+    AttendWork work;
+    const freqkv_status ws = attend_work_for(ctx, plan, l.batch, l.kv_heads * q_heads_per_kv, l.capacity, 0, stream, &work);
+    if (ws != FREQKV_OK) return ws;
+    int32_t launched = 0;
+    cudaError_t e;
+    {
+        TransformTimer timer(ctx, stream);
+        e = launch_attend_q8(q8_view(l, k, v, k_scale, v_scale), l.batch, layer, q, out, q_heads_per_kv, lens, table, scale, plan, work.partial,
+                             work.tickets, &launched, stream);
+    }
+    ctx->kernels_launched += launched;
+    return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "attend_decode_q8");
 }
 
 }  // extern "C"

@@ -22,17 +22,14 @@
 #include <algorithm>
 #include <cmath>
 
-#include <cuda_fp16.h>
-
 #include "attend.cuh"
+#include "attend_dev.cuh"
 
 namespace freqkv {
 namespace {
 
 constexpr int THREADS = 256;
 constexpr int RESYNC = 32;          // rows between two exact reloads of cos/sin
-constexpr float NEG = -1.0e30f;     // "minus infinity" that stays finite under subtraction
-constexpr int PART = 132;           // floats per partial: max, sum, 2 unused, 128 weighted channels
 
 struct AttendParams {
     const void* k;
@@ -50,28 +47,6 @@ struct AttendParams {
     uint16_t tiles[ATTEND_MAX_BATCH];  // of 16 rows in one split of each sequence
 };
 
-// Loads of queries, keys and values.  The kernel may start while the grid that writes them still runs (see wait_for_previous_grid),
-// so they are not constant for its whole life, which the read-only path (ld.global.nc, __ldg) asks for.  volatile: the loads stay
-// behind the wait and in the order they are written in, all of a round first -- 4 layers of 16 x 32 heads x 4096 rows take
-// 714 us with them as with __ldg, but plain loads, which ptxas moves next to their uses, 5 % more.
-__device__ __forceinline__ uint2 load(const uint2* p)
-{
-    uint2 v;
-    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ uint4 load(const uint4* p)
-{
-    uint4 v;
-    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ float4 load(const float4* p)
-{
-    float4 v;
-    asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
-    return v;
-}
 __device__ __forceinline__ void load4(const __nv_bfloat16* p, float (&o)[4])
 {
     const uint2 u = load(reinterpret_cast<const uint2*>(p));
@@ -131,22 +106,6 @@ __device__ __forceinline__ void unpack(const RawRow<float>& r, float (&klo)[4], 
     khi[0] = r.khi.x; khi[1] = r.khi.y; khi[2] = r.khi.z; khi[3] = r.khi.w;
     v[0] = r.v0.x; v[1] = r.v0.y; v[2] = r.v0.z; v[3] = r.v0.w;
     v[4] = r.v1.x; v[5] = r.v1.y; v[6] = r.v1.z; v[7] = r.v1.w;
-}
-
-// 2^x on the special-function unit (2 ulp; the arguments here are <= 0).
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Rotate the pair (lo, hi) by the angle whose cosine and sine are cs.
-__device__ __forceinline__ void rotate(float& lo, float& hi, float2 cs)
-{
-    const float a = lo * cs.x - hi * cs.y, b = hi * cs.x + lo * cs.y;
-    lo = a;
-    hi = b;
 }
 
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
@@ -217,15 +176,6 @@ __device__ __forceinline__ void merge_splits(const AttendParams& p, int32_t b, i
             store1(out + 3, acc.w / sum);
         }
     }
-}
-
-// The kernels are launched with programmatic stream serialization (see launch_attention): the CTAs of the next launch may
-// take their places while the last ones of this launch run, and wait here, before any access to memory, until that
-// grid has completed and its writes are visible.
-__device__ __forceinline__ void wait_for_previous_grid()
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // TICKETS: the last CTA of a group merges its splits (AttendParams::tickets); else attend_merge_kernel follows.  (As a branch
@@ -447,6 +397,7 @@ __global__ void __launch_bounds__(THREADS, (G <= 4 ? 2 : 1)) attend_partial_kern
 // 32 accumulators per thread instead of 64 (heads on M would waste half of them on padding) let
 // three CTAs of four warps share an SM.  Warps, then splits, are merged as in the CUDA-core kernel.
 constexpr int MMA_WARPS = 4, MMA_THREADS = 32 * MMA_WARPS, MMA_CTAS_PER_SM = 3;
+static_assert(MMA_CTAS_PER_SM <= ATTEND_MOST_CTAS_PER_SM, "tickets");
 constexpr int TILE_ROWS = 16;
 constexpr int TILE_BYTES = TILE_ROWS * 256;                   // 16 rows x 128 two-byte values
 constexpr int MMA_STAGES = 2;
@@ -460,51 +411,6 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool v
 {
     const int bytes = valid ? 16 : 0;  // 0 source bytes: the 16 destination bytes are zero-filled
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(addr));
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t addr, uint32_t (&r)[4])
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(addr));
-}
-// 8x8 transpose of 16-bit values held one row per 4 lanes (the ldmatrix fragment layout).
-__device__ __forceinline__ uint32_t transpose_8x8(uint32_t a)
-{
-    uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
-    return d;
-}
-// D += A B, m16n8k16, A row-major, B column-major, fp32 accumulate; bf16 or fp16 operands.
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
 }
 
 template <int G, bool TICKETS>
@@ -869,11 +775,9 @@ constexpr int32_t MIN_ROWS = 192, MOST_SPLITS = 64;
 // chip; one with many groups takes long chunks that fill their last wave.  Measured, us a layer, against two splits
 // of at least 1024 rows: 1 sequence x 8 KV heads x 2611 rows 28.7 -> 13.2 (128 rows 13.4, 256 rows 13.5), 4 x 8 heads of up
 // to 1990 rows 40.7 -> 16.4, 8 x 8 heads of 4099 to 8192 rows 48.9 -> 43.4; OVERHEAD_ROWS 32 and 192 give the same.
-AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int32_t q_heads_per_kv, int32_t dtype, int sm_count)
+AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int64_t resident)
 {
     constexpr int32_t OVERHEAD_ROWS = 96, MOST_ROWS = 0xffff * 16;  // a split's tiles are 16 bits
-    const bool tensor_cores = dtype == FREQKV_BF16 && q_heads_per_kv >= 2;
-    const int64_t resident = (int64_t)sm_count * (tensor_cores ? MMA_CTAS_PER_SM : q_heads_per_kv <= 4 ? 2 : 1);
     const int32_t longest = *std::max_element(lens, lens + batch);
     AttendPlan plan = {};
     int64_t best_cost = -1;
@@ -891,10 +795,16 @@ AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int
     return plan;
 }
 
+int64_t attend_resident(int32_t q_heads_per_kv, int32_t dtype, int sm_count)
+{
+    const bool tensor_cores = dtype == FREQKV_BF16 && q_heads_per_kv >= 2;
+    return (int64_t)sm_count * (tensor_cores ? MMA_CTAS_PER_SM : q_heads_per_kv <= 4 ? 2 : 1);
+}
+
 int32_t attend_most_splits(int32_t longest) { return std::max(1, std::min(longest / MIN_ROWS + 1, MOST_SPLITS)); }
 
 // One wave of CTAs holds at most so many (sequence, kv head) groups; whole 256 bytes, so that what follows is aligned.
-size_t attend_ticket_bytes(int sm_count) { return ((size_t)sm_count * MMA_CTAS_PER_SM * sizeof(int32_t) + 255) & ~(size_t)255; }
+size_t attend_ticket_bytes(int sm_count) { return ((size_t)sm_count * ATTEND_MOST_CTAS_PER_SM * sizeof(int32_t) + 255) & ~(size_t)255; }
 
 size_t attend_partial_bytes(int32_t splits, int32_t batch, int32_t q_heads)
 {

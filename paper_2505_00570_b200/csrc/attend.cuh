@@ -5,6 +5,7 @@
 namespace freqkv {
 
 constexpr int ATTEND_MAX_BATCH = 128;  // sequences per launch (lengths travel as kernel arguments)
+constexpr int ATTEND_MOST_CTAS_PER_SM = 4;
 
 bool attend_supported(int32_t head_dim, int32_t q_heads_per_kv);
 // How the rows of every (sequence, kv head) are split.
@@ -14,7 +15,9 @@ struct AttendPlan {
     bool one_wave;    // all CTAs are resident at once
     bool captured;    // the launches go into a graph: no tickets, no overlap with the launch before
 };
-AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int32_t q_heads_per_kv, int32_t dtype, int sm_count);
+// `resident`: CTAs that the chip holds at once.
+AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int64_t resident);
+int64_t attend_resident(int32_t q_heads_per_kv, int32_t dtype, int sm_count);
 // No plan for lengths up to `longest` has more splits (unless rows beyond what 64 CTAs can take force them).
 int32_t attend_most_splits(int32_t longest);
 // Work areas: one ticket per (sequence, kv head) of a call whose CTAs are all resident, zero before the first launch and

@@ -1,0 +1,438 @@
+// Decode attention of one new token per sequence over the cache in 8 bits: the attention of attend.cu, positions and all, with
+// keys and values  code * scale.
+//
+// One pass over the codes of the layer, 256 bytes a row of K and V: bound by memory, and at the copy rate an SM has 11 clocks
+// for a row, so what counts next to the loads is the instructions a row takes.  A warp takes tiles of 16 rows:
+//  - Codes go from memory into registers in the layout that the matrix instruction (mma.sync m16n8k16, fp32 accumulation) wants,
+//    without shared memory.  The order of the contraction index is free, so a lane's share of a key row is 16 consecutive
+//    channels and the 16 that RoPE pairs with them (two 16-byte loads), and its share of four value rows is 16 channels each.
+//    The next tile's loads are in flight while a tile is computed.
+//  - Codes become fp16 exactly (e4m3: one conversion of two; int8: a byte permute and a subtraction of two).  For V, whose rows are
+//    the contraction index, the bytes of two rows are interleaved before the conversion.
+//  - RoPE: the score of key row j0 + r (j0 the tile's first row) and the query at len - 1 is  k . R(len - 1 - j0 - r) q, and is
+//    computed as  (R(r) k) . (R(len - 1 - j0) q): the key rows of every tile are turned by the same 16 angles, whose cosines
+//    and sines lie in shared memory as fp16, two channels an instruction; the queries (8 heads, one column of the instruction
+//    each) are turned once a tile, in fp32, straight from the table of the context.
+//  - The block's scale of K multiplies the scores, that of V the softmax weights, which are rounded to fp16 as multiples of
+//    the largest V scale so far (`vref`), so that any scales' range will do.
+// Rounding: turned keys and queries to fp16 (cosine, product, sum: 4 roundings of 2^-11 at most each), weights to fp16; all
+// sums fp32; the result once to bf16.
+// Splits of the rows, partial results and their merge as in attend.cu.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "attend_dev.cuh"
+#include "attend_q8.cuh"
+
+namespace freqkv {
+namespace {
+
+constexpr int WARPS = 4, THREADS = 32 * WARPS, CTAS_PER_SM = 3;
+static_assert(CTAS_PER_SM <= ATTEND_MOST_CTAS_PER_SM, "tickets");
+constexpr int TILE = 16;
+constexpr int CS_ROW = 17;   // uint4 per row of the cosines and sines: 8 + 8, and one to spread the rows over the banks
+constexpr int Q_ROW = 36;    // float4 per head: 32, and 4 likewise
+constexpr int O_ROW = 132;   // floats per head of the warps' merge
+
+struct Q8AttendParams {
+    const uint8_t* k;
+    const uint8_t* v;          // codes, moved to the layer
+    const float* k_scale;
+    const float* v_scale;      // moved to the layer
+    int64_t stride_batch, stride_head, stride_token;  // bytes
+    int64_t scale_batch;       // scales from one sequence to the next
+    int32_t blocks, block_shift, kv_heads, g, subs, batch0, total_batch;
+    const __nv_bfloat16* q;    // [batch, kv_heads * g, 128]
+    __nv_bfloat16* out;
+    float* partial;            // [split][batch][kv_heads * g][PART]
+    int32_t* tickets;          // [batch * kv_heads * subs], 0 between launches; null: q8_merge_kernel follows
+    const float2* table;
+    float qscale;              // scale * log2(e)
+    int32_t len[ATTEND_MAX_BATCH];
+    uint16_t tiles[ATTEND_MAX_BATCH];
+};
+
+// Two codes (the low 16 bits) as fp16; four codes as two pairs.
+template <int KIND>
+__device__ __forceinline__ void widen(uint32_t w, __half2& a, __half2& b)
+{
+    if constexpr (KIND == FREQKV_Q8_E4M3) {
+        uint32_t x, y;
+        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(x), "=r"(y) : "r"(w));
+        a = *reinterpret_cast<__half2*>(&x);
+        b = *reinterpret_cast<__half2*>(&y);
+    } else {  // code + 128 as the low byte of 1024 + code + 128, less 1152
+        const uint32_t u = w ^ 0x80808080u, x = __byte_perm(u, 0x64646464u, 0x4140), y = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 off = __float2half2_rn(1152.f);
+        a = __hsub2(*reinterpret_cast<const __half2*>(&x), off);
+        b = __hsub2(*reinterpret_cast<const __half2*>(&y), off);
+    }
+}
+__device__ __forceinline__ uint32_t bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+
+struct Tile {
+    uint4 ka_lo, ka_hi, kb_lo, kb_hi;  // rows gq and gq + 8: channels 16 tq .. and 64 + 16 tq ..
+    uint4 v[4];                        // rows 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9: channels 16 gq ..
+    float ks, vs;                      // the block's scales
+};
+
+// Channel of place t in the partial results: lanes of equal tq write neighbours, see the merge of the warps.
+__device__ __forceinline__ int channel_of(int t) { return (t & 7) * 16 + (t >> 3); }
+
+// All splits of the heads of one CTA's group are there: merge them.  Warps share the heads, and the splits of a head where there
+// are fewer heads than warps.  `sm`: WARPS * (128 + 2) floats.
+__device__ __forceinline__ void q8_merge(const Q8AttendParams& p, int64_t head0, int32_t heads, int32_t n_splits, float* sm)
+{
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int32_t per = heads >= WARPS ? 1 : heads == 1 ? WARPS : WARPS / 2;  // warps a head; with 3 heads, 2 and two rounds
+    const int64_t heads_total = (int64_t)p.total_batch * p.kv_heads * p.g;
+    for (int32_t g0 = 0; g0 < heads; g0 += WARPS / per) {
+        const int32_t g = g0 + warp / per;
+        float mx = NEG, sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (g < heads) {
+            const float* base = p.partial + (head0 + g) * PART;
+            for (int s = lane; s < n_splits; s += 32) mx = fmaxf(mx, __ldcg(base + s * heads_total * PART));
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+#pragma unroll 8
+            for (int s = warp % per; s < n_splits; s += per) {
+                const float* pp = base + s * heads_total * PART;
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp));
+                const float4 o = __ldcg(reinterpret_cast<const float4*>(pp + 4) + lane);
+                const float f = ex2(ml.x - mx);
+                sum = fmaf(ml.y, f, sum);
+                acc.x = fmaf(o.x, f, acc.x);
+                acc.y = fmaf(o.y, f, acc.y);
+                acc.z = fmaf(o.z, f, acc.z);
+                acc.w = fmaf(o.w, f, acc.w);
+            }
+        }
+        if (per > 1) {
+            float* mine = sm + warp * 132;
+            reinterpret_cast<float4*>(mine)[lane] = acc;
+            if (lane == 0) mine[128] = sum;
+            __syncthreads();
+            if (warp % per == 0)
+                for (int w = 1; w < per; ++w) {
+                    const float4 other = reinterpret_cast<const float4*>(sm + (warp + w) * 132)[lane];
+                    acc.x += other.x; acc.y += other.y; acc.z += other.z; acc.w += other.w;
+                    sum += sm[(warp + w) * 132 + 128];
+                }
+            __syncthreads();
+        }
+        if (g < heads && warp % per == 0) {
+            __nv_bfloat16* out = p.out + (head0 + g) * 128;
+            const float inv = 1.f / sum;
+            out[channel_of(4 * lane)] = __float2bfloat16_rn(acc.x * inv);
+            out[channel_of(4 * lane + 1)] = __float2bfloat16_rn(acc.y * inv);
+            out[channel_of(4 * lane + 2)] = __float2bfloat16_rn(acc.z * inv);
+            out[channel_of(4 * lane + 3)] = __float2bfloat16_rn(acc.w * inv);
+        }
+    }
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const __grid_constant__ Q8AttendParams p)
+{
+    wait_for_previous_grid();
+    __shared__ uint4 sm_cs[TILE * CS_ROW];
+    __shared__ float4 sm_q[Q8_HEADS * Q_ROW];
+    __shared__ __align__(16) float sm_o[WARPS * Q8_HEADS * O_ROW];
+    __shared__ float sm_ml[WARPS][Q8_HEADS][2];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, gq = lane / 4, tq = lane % 4;
+    const int32_t sub = (int32_t)blockIdx.y % p.subs, bh = (int32_t)blockIdx.y / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
+    const int32_t len = p.len[b];
+    const int32_t rows = p.tiles[b] * TILE, r0 = (int32_t)blockIdx.x * rows, r1 = min(len, r0 + rows);
+    if (r0 >= len) return;  // a shorter sequence has fewer splits
+    const int32_t n_tiles = (r1 - r0 + TILE - 1) / TILE;
+    const int32_t heads = min(Q8_HEADS, p.g - sub * Q8_HEADS);
+    const int64_t bb = p.batch0 + b, head0 = (bb * p.kv_heads + h) * p.g + sub * Q8_HEADS;
+    const uint8_t* K = p.k + bb * p.stride_batch + h * p.stride_head + 16 * tq;
+    const uint8_t* V = p.v + bb * p.stride_batch + h * p.stride_head + 16 * gq;
+    const float* KS = p.k_scale + bb * p.scale_batch + (int64_t)h * p.blocks;
+    const float* VS = p.v_scale + bb * p.scale_batch + (int64_t)h * p.blocks;
+
+    auto fetch = [&](Tile& t, int32_t tile) {
+        const int32_t j0 = r0 + tile * TILE, last = r1 - 1;  // rows past the end read the last one again; their weights are zero
+        const uint8_t* a = K + (int64_t)min(j0 + gq, last) * p.stride_token;
+        const uint8_t* c = K + (int64_t)min(j0 + gq + 8, last) * p.stride_token;
+        t.ka_lo = load(reinterpret_cast<const uint4*>(a));
+        t.ka_hi = load(reinterpret_cast<const uint4*>(a + 64));
+        t.kb_lo = load(reinterpret_cast<const uint4*>(c));
+        t.kb_hi = load(reinterpret_cast<const uint4*>(c + 64));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            t.v[i] = load(reinterpret_cast<const uint4*>(V + (int64_t)min(j0 + 2 * tq + (i & 1) + (i >> 1) * 8, last) * p.stride_token));
+        t.ks = load1(KS + (j0 >> p.block_shift));
+        t.vs = load1(VS + (j0 >> p.block_shift));
+    };
+    Tile cur, nxt;
+    if (warp < n_tiles) fetch(nxt, warp);
+
+    // queries, scaled, before RoPE: lane (gq, tq) reads channels 16 tq + 4 i and 64 + 16 tq + 4 i of head gq at places 4 i + tq, 16 + 4 i + tq
+    for (int i = tid; i < Q8_HEADS * 32; i += THREADS) {
+        const int head = i / 32, c4 = i % 32, half = c4 / 16, quad = c4 % 16;  // channels 64 half + 4 quad ..
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (head < heads) {
+            const uint2 u = load(reinterpret_cast<const uint2*>(p.q + (head0 + head) * 128 + 4 * c4));
+            x = make_float4(__uint_as_float(u.x << 16) * p.qscale, __uint_as_float(u.x & 0xffff0000u) * p.qscale,
+                            __uint_as_float(u.y << 16) * p.qscale, __uint_as_float(u.y & 0xffff0000u) * p.qscale);
+        }
+        sm_q[head * Q_ROW + half * 16 + (quad & 3) * 4 + quad / 4] = x;
+    }
+    // cosines and sines of rows 0 .. 15
+    for (int i = tid; i < TILE * 64; i += THREADS) {
+        const int r = i / 64, c = i % 64;
+        const float2 cs = p.table ? p.table[i] : make_float2(1.f, 0.f);
+        __half* at = reinterpret_cast<__half*>(sm_cs + r * CS_ROW);
+        at[c] = __float2half_rn(cs.x);
+        at[64 + c] = __float2half_rn(cs.y);
+    }
+    __syncthreads();
+
+    float m_run[2] = {NEG, NEG}, l_run[2] = {0.f, 0.f}, vref = 0.f, vinv = 0.f;
+    float o[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+
+    for (int32_t tile = warp; tile < n_tiles; tile += WARPS) {
+        cur = nxt;
+        if (tile + WARPS < n_tiles) fetch(nxt, tile + WARPS);
+        const int32_t j0 = r0 + tile * TILE;
+
+        // scores of rows gq, gq + 8 and heads 2 tq, 2 tq + 1; four channels and their partners a turn
+        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+        const float4* turn = p.table ? reinterpret_cast<const float4*>(p.table + (int64_t)(len - 1 - j0) * 64 + 16 * tq) : nullptr;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            uint32_t q_lo[2], q_hi[2];
+            {
+                float4 lo = sm_q[gq * Q_ROW + w * 4 + tq], hi = sm_q[gq * Q_ROW + 16 + w * 4 + tq];
+                if (turn) {
+                    const float4 c0 = __ldg(turn + 2 * w), c1 = __ldg(turn + 2 * w + 1);
+                    rotate(lo.x, hi.x, make_float2(c0.x, c0.y));
+                    rotate(lo.y, hi.y, make_float2(c0.z, c0.w));
+                    rotate(lo.z, hi.z, make_float2(c1.x, c1.y));
+                    rotate(lo.w, hi.w, make_float2(c1.z, c1.w));
+                }
+                q_lo[0] = pack2_f16(lo.x, lo.y);
+                q_lo[1] = pack2_f16(lo.z, lo.w);
+                q_hi[0] = pack2_f16(hi.x, hi.y);
+                q_hi[1] = pack2_f16(hi.z, hi.w);
+            }
+            uint32_t a_lo[4], a_hi[4];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {  // rows gq, gq + 8
+                __half2 lo[2], hi[2];
+                widen<KIND>(word(r ? cur.kb_lo : cur.ka_lo, w), lo[0], lo[1]);
+                widen<KIND>(word(r ? cur.kb_hi : cur.ka_hi, w), hi[0], hi[1]);
+                const __half2* cs = reinterpret_cast<const __half2*>(sm_cs + (gq + 8 * r) * CS_ROW + 2 * tq) + 2 * w;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const __half2 c = cs[i], s = cs[32 + i];
+                    a_lo[r + 2 * i] = bits(__hfma2(__hneg2(hi[i]), s, __hmul2(lo[i], c)));
+                    a_hi[r + 2 * i] = bits(__hfma2(lo[i], s, __hmul2(hi[i], c)));
+                }
+            }
+            mma_f16(s0, a_lo, q_lo[0], q_lo[1]);
+            mma_f16(s1, a_hi, q_hi[0], q_hi[1]);
+        }
+        // running softmax, this thread's rows gq and gq + 8
+        const int32_t left = r1 - j0;
+        const bool ok0 = gq < left, ok1 = gq + 8 < left;
+        float corr[2], pw[2][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float sa = (s0[j] + s1[j]) * cur.ks, sb = (s0[2 + j] + s1[2 + j]) * cur.ks;
+            float mx = fmaxf(ok0 ? sa : NEG, ok1 ? sb : NEG);
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+            const float m_new = fmaxf(m_run[j], mx);
+            corr[j] = ex2(m_run[j] - m_new);
+            m_run[j] = m_new;
+            pw[0][j] = ok0 ? ex2(sa - m_new) : 0.f;
+            pw[1][j] = ok1 ? ex2(sb - m_new) : 0.f;
+            l_run[j] = fmaf(l_run[j], corr[j], pw[0][j] + pw[1][j]);
+        }
+        if (cur.vs > vref) {  // the weights' unit grows
+            const float f = vref / cur.vs;
+            corr[0] *= f;
+            corr[1] *= f;
+            vref = cur.vs;
+            vinv = 1.f / vref;
+        }
+        const float unit = cur.vs * vinv;
+        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                o[i][0] *= corr[0];
+                o[i][1] *= corr[1];
+                o[i][2] *= corr[0];
+                o[i][3] *= corr[1];
+            }
+        }
+        const uint32_t p0 = transpose_8x8(pack2_f16(pw[0][0] * unit, pw[0][1] * unit));
+        const uint32_t p1 = transpose_8x8(pack2_f16(pw[1][0] * unit, pw[1][1] * unit));
+        // O^T += V^T P: product i takes channels 16 gq + 2 i and + 1
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t v0 = word(cur.v[0], w), v1 = word(cur.v[1], w), v2 = word(cur.v[2], w), v3 = word(cur.v[3], w);
+            __half2 x[4], y[4];  // channels 4 w + i: rows 2 tq, 2 tq + 1; rows 2 tq + 8, 2 tq + 9
+            widen<KIND>(__byte_perm(v0, v1, 0x5140), x[0], x[1]);
+            widen<KIND>(__byte_perm(v0, v1, 0x7362), x[2], x[3]);
+            widen<KIND>(__byte_perm(v2, v3, 0x5140), y[0], y[1]);
+            widen<KIND>(__byte_perm(v2, v3, 0x7362), y[2], y[3]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t a[4] = {bits(x[2 * i]), bits(x[2 * i + 1]), bits(y[2 * i]), bits(y[2 * i + 1])};
+                mma_f16(o[2 * w + i], a, p0, p1);
+            }
+        }
+    }
+
+    // merge the warps: channel 16 gq + x at place 8 x + gq, so that a store meets no bank twice
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 4);
+        l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 8);
+        l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 16);
+        const int head = 2 * tq + j;
+        if (gq == 0) {
+            sm_ml[warp][head][0] = m_run[j];
+            sm_ml[warp][head][1] = l_run[j];
+        }
+        float* at = sm_o + (warp * Q8_HEADS + head) * O_ROW + gq;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            at[16 * i] = o[i][j] * vref;
+            at[16 * i + 8] = o[i][2 + j] * vref;
+        }
+    }
+    __syncthreads();
+    const int32_t n_splits = (len + rows - 1) / rows;
+    for (int32_t g = 0; g < heads; ++g) {
+        float mn = NEG, sum = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) mn = fmaxf(mn, sm_ml[w][g][0]);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = ex2(sm_ml[w][g][0] - mn);
+            sum = fmaf(sm_ml[w][g][1], f, sum);
+            acc = fmaf(sm_o[(w * Q8_HEADS + g) * O_ROW + tid], f, acc);
+        }
+        if (n_splits == 1) {
+            p.out[(head0 + g) * 128 + channel_of(tid)] = __float2bfloat16_rn(acc / sum);
+            continue;
+        }
+        float* part = p.partial + (((int64_t)blockIdx.x * p.total_batch + bb) * p.kv_heads * p.g + h * p.g + sub * Q8_HEADS + g) * PART;
+        part[4 + tid] = acc;
+        if (tid == 0) {
+            part[0] = mn;
+            part[1] = sum;
+        }
+    }
+    if (!p.tickets || n_splits == 1) return;
+    __shared__ int32_t is_last;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+        int32_t* t = p.tickets + (bb * p.kv_heads + h) * p.subs + sub;
+        const int32_t last = atomicAdd(t, 1) == n_splits - 1;
+        if (last) *t = 0;  // for the next launch
+        is_last = last;
+    }
+    __syncthreads();
+    if (!is_last) return;
+    __threadfence();
+    q8_merge(p, head0, heads, n_splits, sm_o);
+}
+
+// One block per (sequence, kv head, group of heads) with several splits.
+__global__ void __launch_bounds__(THREADS) q8_merge_kernel(const __grid_constant__ Q8AttendParams p)
+{
+    __shared__ __align__(16) float sm[WARPS * 132];
+    const int32_t sub = (int32_t)blockIdx.x % p.subs, bh = (int32_t)blockIdx.x / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
+    const int32_t rows = p.tiles[b] * TILE, n_splits = (p.len[b] + rows - 1) / rows;
+    if (n_splits == 1) return;  // written by the CTA itself
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched with programmatic stream serialization
+    q8_merge(p, ((int64_t)(p.batch0 + b) * p.kv_heads + h) * p.g + sub * Q8_HEADS, min(Q8_HEADS, p.g - sub * Q8_HEADS), n_splits, sm);
+}
+
+cudaError_t launch(void (*kernel)(const Q8AttendParams), dim3 grid, const Q8AttendParams& prm, bool overlap, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, prm);
+}
+
+}  // namespace
+
+int64_t attend_q8_resident(int sm_count) { return (int64_t)sm_count * CTAS_PER_SM; }
+
+cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, const void* q, void* out, int32_t g, const int32_t* lens,
+                             const float2* table, float scale, const AttendPlan& plan, float* partial, int32_t* tickets,
+                             int32_t* launched, cudaStream_t stream)
+{
+    *launched = 0;
+    Q8AttendParams prm;
+    const int64_t scale_layer = (int64_t)layer * cache.kv_heads * cache.blocks;
+    prm.k = static_cast<const uint8_t*>(cache.codes[0]) + layer * cache.stride_layer;
+    prm.v = static_cast<const uint8_t*>(cache.codes[1]) + layer * cache.stride_layer;
+    prm.k_scale = cache.scales[0] + scale_layer;
+    prm.v_scale = cache.scales[1] + scale_layer;
+    prm.stride_batch = cache.stride_batch;
+    prm.stride_head = cache.stride_head;
+    prm.stride_token = cache.stride_token;
+    prm.scale_batch = (int64_t)cache.layers * cache.kv_heads * cache.blocks;
+    prm.blocks = cache.blocks;
+    prm.block_shift = cache.block_tokens == 16 ? 4 : cache.block_tokens == 32 ? 5 : cache.block_tokens == 64 ? 6 : 7;
+    prm.kv_heads = cache.kv_heads;
+    prm.g = g;
+    prm.subs = q8_head_groups(g);
+    prm.total_batch = batch;
+    prm.q = static_cast<const __nv_bfloat16*>(q);
+    prm.out = static_cast<__nv_bfloat16*>(out);
+    prm.partial = partial;
+    // (a captured launch takes no tickets and does not overlap the one before: see launch_attend)
+    prm.tickets = plan.one_wave && !plan.captured ? tickets : nullptr;
+    prm.table = table;
+    prm.qscale = scale * 1.4426950408889634f;
+    // sequences per launch: their lengths travel as kernel arguments, their groups are rows of the grid
+    const int32_t groups = cache.kv_heads * prm.subs, per_launch = std::max(1, std::min(ATTEND_MAX_BATCH, 65535 / groups));
+    for (int32_t b0 = 0; b0 < batch; b0 += per_launch) {
+        const int32_t nb = std::min(per_launch, batch - b0);
+        prm.batch0 = b0;
+        int32_t splits = 1;
+        for (int32_t i = 0; i < nb; ++i) {
+            const int32_t len = lens[b0 + i], n = (len + plan.chunk - 1) / plan.chunk;
+            prm.len[i] = len;
+            prm.tiles[i] = (uint16_t)(((len + n - 1) / n + 15) / 16);
+            splits = std::max(splits, n);
+        }
+        const cudaError_t e = launch(cache.kind == FREQKV_Q8_INT8 ? attend_q8_kernel<FREQKV_Q8_INT8> : attend_q8_kernel<FREQKV_Q8_E4M3>,
+                                     dim3((unsigned)splits, (unsigned)(nb * groups)), prm, !plan.captured, stream);
+        if (e != cudaSuccess) return e;
+        ++*launched;
+        if (!prm.tickets && splits > 1) {
+            const cudaError_t me = launch(q8_merge_kernel, dim3((unsigned)(nb * groups)), prm, true, stream);
+            if (me != cudaSuccess) return me;
+            ++*launched;
+        }
+    }
+    return cudaSuccess;
+}
+
+}  // namespace freqkv

@@ -48,7 +48,7 @@ struct freqkv_ctx {
     void* attend_work = nullptr;  // attend_ticket_bytes of tickets, then the splits' partials
     size_t attend_work_bytes = 0;
     int32_t* attend_lens = nullptr;  // host: the last call's lengths; what else its split of the rows follows from; that split
-    int32_t attend_lens_room = 0, attend_key[4] = {0, 0, 0, 0};
+    int32_t attend_lens_room = 0, attend_key[3] = {0, 0, 0};
     freqkv::AttendPlan attend_last = {};
     bool attend_tickets_clear = false;  // zeroed on a stream that later calls are ordered behind
     void* prefill_keys = nullptr;     // rotated keys of one layer, fp16
@@ -84,6 +84,7 @@ struct DeviceGuard {
 struct WorkOrder {
     freqkv_ctx* ctx;
     cudaStream_t stream;
+    bool captured;  // a captured call enqueues nothing now, and its replays are the caller's to order
     WorkOrder(freqkv_ctx* c, cudaStream_t s);
     ~WorkOrder();
 };
@@ -97,6 +98,17 @@ freqkv_status check_tensors(const freqkv_layout& l, const void* k, const void* v
 int64_t span_elements(const freqkv_layout& l);
 // The context's cos/sin table of `rope_base`, of `capacity` rows at least; *table stays null when RoPE is off.
 freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base, cudaStream_t stream, const float2** table);
+
+// The split of the rows of a decode attention of `groups` (kv head, ...) groups a sequence; the work area of the call: tickets, the
+// splits' partials of q_heads heads a sequence, `more` bytes for the caller (256-byte aligned).
+AttendPlan attend_plan_for(freqkv_ctx* ctx, int32_t batch, int32_t groups, int64_t resident, const int32_t* lens);
+struct AttendWork {
+    int32_t* tickets;
+    float* partial;
+    char* more;
+};
+freqkv_status attend_work_for(freqkv_ctx* ctx, const AttendPlan& plan, int32_t batch, int32_t q_heads, int32_t capacity, size_t more,
+                              cudaStream_t stream, AttendWork* out);
 
 #define FREQKV_CUDA(ctx, call)                                             \
     do {                                                                   \
