@@ -338,6 +338,15 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
                                       const float* v_scale, int32_t layer, const void* q, void* out, int32_t q_heads_per_kv,
                                       const int32_t* lens, float rope_base, float scale, void* cuda_stream);
 
+/* freqkv_attend_prefill over an 8-bit cache (the chunk's rows appended already): the same causal attention, layout of q and out
+ * and positions, with keys and values  code * scale.  Any q_heads_per_kv from 1 to 64.  Turned keys, scaled queries, values (as multiples of a power of
+ * two near their head's largest scale) and softmax weights are rounded to fp16, sums are fp32, the result is rounded once to bf16;  turned keys
+ * and  scale * log2(e) * q  must stay below 65504.  Work areas (keys and values of one layer in fp16, the chunk's queries) and capture as for
+ * freqkv_attend_prefill.  Errors: those of freqkv_attend_decode_q8, with lengths in [n_new, capacity] and n_new >= 1. */
+freqkv_status freqkv_attend_prefill_q8(freqkv_ctx* ctx, const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                       const float* v_scale, int32_t layer, const void* q, void* out, int32_t q_heads_per_kv,
+                                       int32_t n_new, const int32_t* lens, float rope_base, float scale, void* cuda_stream);
+
 /* Instrumentation for benchmarks.  With timing enabled every compression records a CUDA event
  * pair on the caller's stream around its transform kernel (the projection / fast-transform
  * launch, not the copy-back or table builders; the folded fp32 product's three launches together).  freqkv_get_timing waits for the recorded
@@ -418,7 +427,7 @@ freqkv_status freqkv_check_append_q8(const freqkv_q8_layout* layout, const void*
                                      const int32_t* lens);
 freqkv_status freqkv_check_attend_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
                                      const float* v_scale, int32_t layer, const void* q, const void* out, int32_t q_heads_per_kv,
-                                     const int32_t* lens);
+                                     int32_t n_new, const int32_t* lens);  /* n_new = 1: freqkv_attend_decode_q8 */
 /* (of freqkv_quantize and freqkv_dequantize alike) */
 freqkv_status freqkv_check_quantize(const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
                                     const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,

@@ -34,7 +34,7 @@ EXPORTS = [
     "freqkv_decode_graph_create", "freqkv_decode_graph_launch", "freqkv_decode_graph_destroy",
     "freqkv_set_wait_limit", "freqkv_selftest_bounded_wait", "freqkv_fast_plan_apply_host", "freqkv_set_fast_family", "freqkv_gemm_fold_levels", "freqkv_gemm_blocks",
     "freqkv_append_q8", "freqkv_quantize", "freqkv_dequantize", "freqkv_check_append_q8", "freqkv_check_quantize",
-    "freqkv_attend_decode_q8", "freqkv_check_attend_q8",
+    "freqkv_attend_decode_q8", "freqkv_check_attend_q8", "freqkv_attend_prefill_q8",
 ]
 NOALLOC_MAX_BASIS_ELEMS = 1 << 20
 NOALLOC_STAGING_BYTES = 4 << 20
@@ -125,7 +125,9 @@ def lib() -> ctypes.CDLL:
         L.freqkv_check_quantize.argtypes = [LP, c_void_p, c_void_p, I32P, QP, *four]
         L.freqkv_attend_decode_q8.argtypes = [c_void_p, QP, *four, c_int32, c_void_p, c_void_p, c_int32, I32P, ctypes.c_float,
                                               ctypes.c_float, c_void_p]
-        L.freqkv_check_attend_q8.argtypes = [QP, *four, c_int32, c_void_p, c_void_p, c_int32, I32P]
+        L.freqkv_attend_prefill_q8.argtypes = [c_void_p, QP, *four, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P, ctypes.c_float,
+                                               ctypes.c_float, c_void_p]
+        L.freqkv_check_attend_q8.argtypes = [QP, *four, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P]
         L.freqkv_last_error.argtypes = [c_void_p]
         L.freqkv_last_error.restype = c_char_p
         L.freqkv_status_string.argtypes = [c_int]
@@ -519,6 +521,21 @@ class Context:
         st = lib().freqkv_attend_decode_q8(self._h, cache._ref, *cache._ptrs, layer, q.data_ptr(), out.data_ptr(),
                                            q.shape[1] // lay.kv_heads, (c_int32 * lay.batch)(*lens), rope_base, scale, _stream_ptr(stream))
         self._check(st, "freqkv_attend_decode_q8")
+        return out
+
+    def attend_prefill_q8(self, cache: Q8Cache, layer: int, q: torch.Tensor, lens: list[int], rope_base: float = 10000.0,
+                          scale: float = 0.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """``attend_prefill`` over an 8-bit cache: the chunk's rows are appended already.  ``q``: dense bf16
+        [batch, q_heads, n_new, 128], before RoPE.  Returns ``out``."""
+        lay = cache.layout
+        if q.dim() != 4 or not q.is_contiguous() or q.dtype != torch.bfloat16 or q.shape[0] != lay.batch or \
+                q.shape[3] != lay.head_dim or q.shape[1] % lay.kv_heads != 0 or len(lens) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "q must be dense bf16 [batch, q_heads, n_new, head_dim], lens one entry per sequence")
+        out = self._out(q, out)
+        st = lib().freqkv_attend_prefill_q8(self._h, cache._ref, *cache._ptrs, layer, q.data_ptr(), out.data_ptr(),
+                                            q.shape[1] // lay.kv_heads, q.shape[2], (c_int32 * lay.batch)(*lens), rope_base, scale,
+                                            _stream_ptr(stream))
+        self._check(st, "freqkv_attend_prefill_q8")
         return out
 
     @staticmethod

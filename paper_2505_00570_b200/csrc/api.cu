@@ -190,6 +190,29 @@ freqkv_status attend_work_for(freqkv_ctx* ctx, const AttendPlan& plan, int32_t b
     return FREQKV_OK;
 }
 
+freqkv_status prefill_scratch(freqkv_ctx* ctx, size_t key_bytes, size_t query_bytes)
+{
+    struct Grow { void** p; size_t* have; size_t need; };
+    const Grow scratch[2] = {{&ctx->prefill_keys, &ctx->prefill_keys_bytes, key_bytes}, {&ctx->prefill_queries, &ctx->prefill_queries_bytes, query_bytes}};
+    for (const Grow& s : scratch) {
+        if (s.need <= *s.have) continue;
+        if (*s.p) {
+            FREQKV_CUDA(ctx, cudaDeviceSynchronize());  // an enqueued launch may still use the old buffer
+            cudaFree(*s.p);
+            *s.p = nullptr;
+            *s.have = 0;
+        }
+        if (cudaMalloc(s.p, s.need) != cudaSuccess) {
+            cudaGetLastError();
+            *s.p = nullptr;
+            ctx->last_error = "out of device memory for the prefill attention scratch";
+            return FREQKV_ERR_ALLOC;
+        }
+        *s.have = s.need;
+    }
+    return FREQKV_OK;
+}
+
 }  // namespace freqkv
 
 namespace {
@@ -1178,25 +1201,8 @@ freqkv_status freqkv_attend_prefill(freqkv_ctx* ctx, const freqkv_layout* layout
     const float2* table = nullptr;
     const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
-    struct Grow { void** p; size_t* have; size_t need; };
-    const Grow scratch[2] = {{&ctx->prefill_keys, &ctx->prefill_keys_bytes, prefill_key_scratch_bytes(l)},
-                             {&ctx->prefill_queries, &ctx->prefill_queries_bytes, prefill_query_scratch_bytes(l, q_heads_per_kv, n_new)}};
-    for (const Grow& s : scratch) {
-        if (s.need <= *s.have) continue;
-        if (*s.p) {
-            FREQKV_CUDA(ctx, cudaDeviceSynchronize());  // an enqueued launch may still use the old buffer
-            cudaFree(*s.p);
-            *s.p = nullptr;
-            *s.have = 0;
-        }
-        if (cudaMalloc(s.p, s.need) != cudaSuccess) {
-            cudaGetLastError();
-            *s.p = nullptr;
-            ctx->last_error = "out of device memory for the prefill attention scratch";
-            return FREQKV_ERR_ALLOC;
-        }
-        *s.have = s.need;
-    }
+    const freqkv_status gs = prefill_scratch(ctx, prefill_key_scratch_bytes(l), prefill_query_scratch_bytes(l, q_heads_per_kv, n_new));
+    if (gs != FREQKV_OK) return gs;
     const char* why = nullptr;
     int32_t launched = 0;
     cudaError_t e;

@@ -4,6 +4,7 @@
 
 #include "ctx.cuh"
 #include "attend_q8.cuh"
+#include "prefill.cuh"
 #include "q8.cuh"
 
 using namespace freqkv;
@@ -202,17 +203,17 @@ freqkv_status freqkv_dequantize(freqkv_ctx* ctx, const freqkv_q8_layout* layout,
 
 freqkv_status freqkv_check_attend_q8(const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
                                      const float* v_scale, int32_t layer, const void* q, const void* out, int32_t q_heads_per_kv,
-                                     const int32_t* lens)
+                                     int32_t n_new, const int32_t* lens)
 {
     if (!lens) return FREQKV_ERR_INVALID_ARG;
     const freqkv_status st = check_q8(layout, k, v, k_scale, v_scale);
     if (st != FREQKV_OK) return st;
     if (!q || !out || q == out) return FREQKV_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)out) & 15) return FREQKV_ERR_UNSUPPORTED;
-    if (layer < 0 || layer >= layout->layers || q_heads_per_kv < 1) return FREQKV_ERR_INVALID_ARG;
+    if (layer < 0 || layer >= layout->layers || q_heads_per_kv < 1 || n_new < 1) return FREQKV_ERR_INVALID_ARG;
     if (layout->head_dim != 128 || q_heads_per_kv > 64 || (int64_t)layout->kv_heads * q_heads_per_kv > 65535) return FREQKV_ERR_UNSUPPORTED;
     for (int32_t b = 0; b < layout->batch; ++b)
-        if (lens[b] < 1 || lens[b] > layout->capacity) return FREQKV_ERR_INVALID_ARG;
+        if (lens[b] < n_new || lens[b] > layout->capacity) return FREQKV_ERR_INVALID_ARG;
     return FREQKV_OK;
 }
 
@@ -221,7 +222,7 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
                                       const int32_t* lens, float rope_base, float scale, void* cuda_stream)
 {
     if (!ctx) return FREQKV_ERR_INVALID_ARG;
-    const freqkv_status st = freqkv_check_attend_q8(layout, k, v, k_scale, v_scale, layer, q, out, q_heads_per_kv, lens);
+    const freqkv_status st = freqkv_check_attend_q8(layout, k, v, k_scale, v_scale, layer, q, out, q_heads_per_kv, 1, lens);
     if (st != FREQKV_OK) return st;
     if (!(scale == scale) || !(rope_base == rope_base)) return FREQKV_ERR_INVALID_ARG;  // NaN
     const freqkv_q8_layout& l = *layout;
@@ -247,6 +248,43 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
     }
     ctx->kernels_launched += launched;
     return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "attend_decode_q8");
+}
+
+freqkv_status freqkv_attend_prefill_q8(freqkv_ctx* ctx, const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
+                                       const float* v_scale, int32_t layer, const void* q, void* out, int32_t q_heads_per_kv,
+                                       int32_t n_new, const int32_t* lens, float rope_base, float scale, void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_attend_q8(layout, k, v, k_scale, v_scale, layer, q, out, q_heads_per_kv, n_new, lens);
+    if (st != FREQKV_OK) return st;
+    if (!(scale == scale) || !(rope_base == rope_base)) return FREQKV_ERR_INVALID_ARG;  // NaN
+    const freqkv_q8_layout& l = *layout;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    WorkOrder order(ctx, stream);
+    if (scale <= 0.f) scale = 1.0f / sqrtf((float)l.head_dim);
+    const float2* table = nullptr;
+    const freqkv_status ts = rope_table_for(ctx, std::max(l.capacity, 16), rope_base, stream, &table);
+    if (ts != FREQKV_OK) return ts;
+    const Q8View view = q8_view(l, k, v, k_scale, v_scale);
+    const freqkv_status gs = prefill_scratch(ctx, prefill_q8_scratch_bytes(view, l.batch, l.capacity),
+                                             (size_t)l.batch * l.kv_heads * q_heads_per_kv * n_new * 256);
+    if (gs != FREQKV_OK) return gs;
+    const char* why = nullptr;
+    int32_t launched = 0;
+    cudaError_t e;
+    {
+        TransformTimer timer(ctx, stream);
+        e = launch_prefill_q8(view, l.batch, l.capacity, layer, q, out, q_heads_per_kv, n_new, lens, table, scale, ctx->prefill_keys,
+                              ctx->prefill_queries, ctx->status_dev, ctx->gemm.wait_limit_ns, &why, &launched, stream);
+    }
+    ctx->kernels_launched += launched;
+    if (e == cudaSuccess) return FREQKV_OK;
+    if (!why) return cuda_fail(ctx, e, "attend_prefill_q8");
+    cudaGetLastError();
+    ctx->last_error = why;
+    return e == cudaErrorNotSupported ? FREQKV_ERR_UNSUPPORTED : FREQKV_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -110,6 +110,9 @@ struct AttendWork {
 freqkv_status attend_work_for(freqkv_ctx* ctx, const AttendPlan& plan, int32_t batch, int32_t q_heads, int32_t capacity, size_t more,
                               cudaStream_t stream, AttendWork* out);
 
+// Makes the prefill attention's two scratch buffers at least so large.
+freqkv_status prefill_scratch(freqkv_ctx* ctx, size_t key_bytes, size_t query_bytes);
+
 #define FREQKV_CUDA(ctx, call)                                             \
     do {                                                                   \
         const cudaError_t e__ = (call);                                    \

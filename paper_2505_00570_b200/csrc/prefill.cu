@@ -34,10 +34,13 @@
 //              independent of the reference.  Value rows past the cache length (stale cache
 //              contents, possibly not finite) are zeroed in shared memory before they are used.
 //     At the end the softmax threads read O, divide by the row sums and store bf16 rows.
+// Over a cache in 8 bits pass 1 also writes the layer's values, in fp16, and pass 2 reads them there; its weights are
+// fp16, too (codes are exact in fp16 and weights below 2^8 keep 11 bits, where bf16 would round both to 8).
 // Every barrier wait is bounded in time; a wait that runs out sets a status bit and an abort flag
 // that ends all roles, after which the CTA lets copies in flight land and frees its tensor memory.
 #include <cuda.h>
 #include <cuda_fp16.h>
+#include <cuda_fp8.h>
 
 #include <algorithm>
 
@@ -65,6 +68,7 @@ constexpr float RESCALE_STEP = 8.f;  // log2 of the largest weight the lazy refe
 
 struct PrefillParams {
     int32_t n_new, kv_heads, g, layer, batch0, batch_count, q_tiles;
+    const float* unit;  // value scratch of an 8-bit cache: [batch * kv_heads], what one is worth
     __nv_bfloat16* out;  // [batch, kv_heads * g, n_new, 128]
     int32_t* status;
     unsigned long long wait_limit_ns;  // bound of every mbarrier wait
@@ -181,6 +185,7 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes,
 // Instruction descriptors, kind::f16, D fp32, M = 128.
 // Scores (N = 64 keys): A and B fp16, both K-major.  Values (N = 128 channels): A and B bf16, A K-major, B MN-major.
 constexpr uint32_t IDESC_QK = (1u << 4) | (0u << 7) | (0u << 10) | (0u << 15) | (0u << 16) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t IDESC_PV_F16 = (1u << 4) | (0u << 7) | (0u << 10) | (0u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);  // values of an 8-bit cache
 constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (0u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 
 __device__ __forceinline__ void umma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -322,7 +327,111 @@ __global__ void __launch_bounds__(256) prefill_rope_kernel(const RopeJob job)
     }
 }
 
+// ---- pass 1 over a cache in 8 bits ----
+//
+// Jobs as above, and one more for each key row: its value row.  Keys are turned in fp32 from  code * scale.  Values go to
+// scratch in fp16 as multiples of a power of two that holds the largest scale of the head, so that any scale's range
+// will do (code * scale / unit is at most 448, rounded to 2^-11 for INT8, exact for E4M3 but for scales 2^-14 below the largest).
+struct Q8RopeJob {
+    const uint8_t* k;
+    const uint8_t* v;          // codes, moved to the layer
+    const float* k_scale;
+    const float* v_scale;      // moved to the layer
+    int64_t stride_batch, stride_head, stride_token, scale_batch;
+    int32_t blocks, block_shift, kind;
+    const __nv_bfloat16* q;
+    __half* k_out;             // [batch * kv_heads][capacity][128]
+    __half* v_out;             // the same
+    float* unit;               // [batch * kv_heads]
+    __half* q_out;
+    const float2* table;
+    float qscale;
+    int32_t kv_heads, heads_q, n_new, capacity, k_rows, batch0, batch_count;
+    int32_t len[PREFILL_MAX_BATCH];
+};
+
+__device__ __forceinline__ float code_value(uint32_t code, int32_t kind)
+{
+    return kind == FREQKV_Q8_INT8 ? (float)(int8_t)code : __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+
+__global__ void __launch_bounds__(256) prefill_q8_rope_kernel(const __grid_constant__ Q8RopeJob job)
+{
+    __shared__ float sm_max[8];
+    const int l16 = threadIdx.x % 16, c0 = 4 * l16;
+    const int32_t k_slices = job.batch_count * job.kv_heads;
+    const bool is_key = (int32_t)blockIdx.y < k_slices;
+    const int32_t slice = is_key ? (int32_t)blockIdx.y : (int32_t)blockIdx.y - k_slices;
+    const int32_t heads = is_key ? job.kv_heads : job.heads_q, b = slice / heads, hh = slice % heads;
+    const int32_t rows = is_key ? job.k_rows : job.n_new, len = job.len[b];
+    if ((int32_t)blockIdx.x * 64 >= rows) return;
+    const int64_t bb = job.batch0 + b;
+    float v_mul = 0.f;
+    if (is_key) {  // the largest scale of V over the rows in use, and the power of two that holds it
+        const float* vs = job.v_scale + bb * job.scale_batch + (int64_t)hh * job.blocks;
+        float m = 0.f;
+        for (int32_t i = threadIdx.x; i <= (len - 1) >> job.block_shift; i += 256) m = fmaxf(m, vs[i]);
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+        if (threadIdx.x % 32 == 0) sm_max[threadIdx.x / 32] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, sm_max[i]);
+        const uint32_t e = min(max((__float_as_uint(m) + 0x7fffffu) >> 23, 1u), 253u);  // 2^(e - 127) >= m
+        v_mul = __uint_as_float((254u - e) << 23);
+        if (blockIdx.x == 0 && threadIdx.x == 0) job.unit[bb * job.kv_heads + hh] = __uint_as_float(e << 23);
+    }
+    const int32_t pos0 = is_key ? 0 : len - job.n_new;
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+        const int32_t row = (int32_t)blockIdx.x * 64 + (threadIdx.x / 16) * 4 + i4;
+        if (row >= rows) break;
+        float lo[4] = {0.f, 0.f, 0.f, 0.f}, hi[4] = {0.f, 0.f, 0.f, 0.f}, vv[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (!is_key) {
+            const __nv_bfloat16* src = job.q + ((bb * job.heads_q + hh) * job.n_new + row) * 128;
+            const uint2 a = __ldg(reinterpret_cast<const uint2*>(src + c0)), c = __ldg(reinterpret_cast<const uint2*>(src + 64 + c0));
+            const uint32_t w[4] = {a.x, a.y, c.x, c.y};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                (i < 2 ? lo : hi)[2 * (i & 1)] = __uint_as_float(w[i] << 16) * job.qscale;
+                (i < 2 ? lo : hi)[2 * (i & 1) + 1] = __uint_as_float(w[i] & 0xffff0000u) * job.qscale;
+            }
+        } else if (row < len) {  // rows from the length on are written as zeros
+            const int64_t at = bb * job.stride_batch + hh * job.stride_head + (int64_t)row * job.stride_token, sc = bb * job.scale_batch + (int64_t)hh * job.blocks + (row >> job.block_shift);
+            const float ks = __ldg(job.k_scale + sc), vs = __ldg(job.v_scale + sc) * v_mul;
+            const uint32_t a = __ldg(reinterpret_cast<const uint32_t*>(job.k + at + c0)), c = __ldg(reinterpret_cast<const uint32_t*>(job.k + at + 64 + c0));
+            const uint2 u = __ldg(reinterpret_cast<const uint2*>(job.v + at + 8 * l16));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lo[i] = code_value(a >> 8 * i & 255u, job.kind) * ks;
+                hi[i] = code_value(c >> 8 * i & 255u, job.kind) * ks;
+                vv[i] = code_value(u.x >> 8 * i & 255u, job.kind) * vs;
+                vv[4 + i] = code_value(u.y >> 8 * i & 255u, job.kind) * vs;
+            }
+        }
+        if (job.table && !(is_key && row >= len)) {
+            const float4* t = reinterpret_cast<const float4*>(job.table + (int64_t)(pos0 + row) * 64 + c0);
+            const float4 t0 = __ldg(t), t1 = __ldg(t + 1);
+            const float cs[4] = {t0.x, t0.z, t1.x, t1.z}, sn[4] = {t0.y, t0.w, t1.y, t1.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = lo[i] * cs[i] - hi[i] * sn[i], y = hi[i] * cs[i] + lo[i] * sn[i];
+                lo[i] = x;
+                hi[i] = y;
+            }
+        }
+        __half* dst = is_key ? job.k_out + ((bb * job.kv_heads + hh) * job.capacity + row) * 128 : job.q_out + ((bb * job.heads_q + hh) * job.n_new + row) * 128;
+        *reinterpret_cast<uint2*>(dst + c0) = make_uint2(pack_f16(lo[0], lo[1]), pack_f16(lo[2], lo[3]));
+        *reinterpret_cast<uint2*>(dst + 64 + c0) = make_uint2(pack_f16(hi[0], hi[1]), pack_f16(hi[2], hi[3]));
+        if (is_key)
+            *reinterpret_cast<uint4*>(job.v_out + ((bb * job.kv_heads + hh) * job.capacity + row) * 128 + 8 * l16) =
+                make_uint4(pack_f16(vv[0], vv[1]), pack_f16(vv[2], vv[3]), pack_f16(vv[4], vv[5]), pack_f16(vv[6], vv[7]));
+    }
+}
+
 // ---- pass 2 ----
+// Q8: values and weights in fp16, values from scratch (map_v: channel, row, slice) whose rows past the length are zeros.
+template <bool Q8>
 __global__ void __launch_bounds__(THREADS, 2)
 prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap map_v, const PrefillParams prm)
@@ -403,8 +512,13 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 tma_load_3d(base + OFF_K + sk * KV_TILE + KV_SLAB, &map_k, k_full(sk), 64, t * BKV, k_slice);
                 if (t >= RING_V && !mbar_wait(v_empty(sv), ((uint32_t)(t / RING_V) - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
                 mbar_expect_tx(v_full(sv), KV_TILE);
-                tma_load_5d(base + OFF_V + sv * KV_TILE, &map_v, v_full(sv), 0, t * BKV, h, prm.layer, prm.batch0 + b);
-                tma_load_5d(base + OFF_V + sv * KV_TILE + KV_SLAB, &map_v, v_full(sv), 64, t * BKV, h, prm.layer, prm.batch0 + b);
+                if constexpr (Q8) {
+                    tma_load_3d(base + OFF_V + sv * KV_TILE, &map_v, v_full(sv), 0, t * BKV, k_slice);
+                    tma_load_3d(base + OFF_V + sv * KV_TILE + KV_SLAB, &map_v, v_full(sv), 64, t * BKV, k_slice);
+                } else {
+                    tma_load_5d(base + OFF_V + sv * KV_TILE, &map_v, v_full(sv), 0, t * BKV, h, prm.layer, prm.batch0 + b);
+                    tma_load_5d(base + OFF_V + sv * KV_TILE + KV_SLAB, &map_v, v_full(sv), 64, t * BKV, h, prm.layer, prm.batch0 + b);
+                }
             }
             if (*abort_flag) {  // let the copies in flight land before this CTA's shared memory goes away
                 const unsigned long long t0 = global_timer_ns();
@@ -441,7 +555,7 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 for (int kk = 0; kk < BKV / 16; ++kk)  // 16 keys per instruction
                     // P: in tensor memory over the first 32 columns of this tile's S buffer, 8 columns per step.
                     // V: MN-major, 16 key rows = 2 KB per step, 64-channel slabs KV_SLAB apart.
-                    umma_ts(tmem_o, tmem_base + (t & 1) * BKV + kk * 8, smem_desc(va + kk * 2048, KV_SLAB, 1024), IDESC_PV, (t | kk) != 0);
+                    umma_ts(tmem_o, tmem_base + (t & 1) * BKV + kk * 8, smem_desc(va + kk * 2048, KV_SLAB, 1024), Q8 ? IDESC_PV_F16 : IDESC_PV, (t | kk) != 0);
                 umma_commit(o_full);
                 umma_commit(v_empty(s));
             }
@@ -494,7 +608,7 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 p0 = ex2(p0);
                 p1 = ex2(p1);
                 s4[j & 3] = add2(s4[j & 3], pair(p0, p1));
-                pk[j] = pack_bf16(p0, p1);
+                pk[j] = Q8 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
             }
             float sum_lo, sum_hi;
             unpair(add2(add2(s4[0], s4[1]), add2(s4[2], s4[3])), sum_lo, sum_hi);
@@ -522,7 +636,7 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             tmem_st32(tmem_base + lane_bits + buf * BKV, pk);
             asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            if (j0 + BKV > len) {  // value rows past the cache length are stale: make them zeros
+            if (!Q8 && j0 + BKV > len) {  // value rows past the cache length are stale: make them zeros
                 if (!mbar_wait(v_full(s), (uint32_t)(t / RING_V) & 1, abort_flag, prm.status, prm.wait_limit_ns)) { alive = false; break; }
                 if (row < BKV && j0 + row >= len) {
                     uint8_t* v_row = aligned + OFF_V + s * KV_TILE + row * 128;
@@ -538,7 +652,7 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         }
         if (alive && mbar_wait(o_full, (n_tiles - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const float inv = 1.f / l_run;
+            const float inv = (Q8 ? __ldcg(prm.unit + (prm.batch0 + b) * prm.kv_heads + h) : 1.f) / l_run;
             const bool store = q0 + row < prm.n_new;
             uint4* out = reinterpret_cast<uint4*>(prm.out + ((((int64_t)(prm.batch0 + b) * heads_q + hq) * prm.n_new + q0 + row) * 128));
 #pragma unroll
@@ -627,6 +741,19 @@ size_t prefill_query_scratch_bytes(const freqkv_layout& l, int32_t q_heads_per_k
     return (size_t)l.batch * l.kv_heads * q_heads_per_kv * n_new * 256;
 }
 
+static cudaError_t set_attributes()
+{
+    static PerDeviceOnce attrs;
+    return attrs.run([] {
+        for (const void* f : {(const void*)prefill_attend_kernel<false>, (const void*)prefill_attend_kernel<true>}) {
+            cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+            if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+    });
+}
+
 cudaError_t launch_prefill(const freqkv_layout& l, const void* k, const void* v, int32_t layer, const void* q, void* out,
                            int32_t g, int32_t n_new, const int32_t* lens_host, const float2* table, float scale,
                            void* key_scratch, void* query_scratch, int32_t* status, unsigned long long wait_limit_ns,
@@ -637,13 +764,7 @@ cudaError_t launch_prefill(const freqkv_layout& l, const void* k, const void* v,
         *error = "cuTensorMapEncodeTiled is not available from this driver";
         return cudaErrorNotSupported;
     }
-    static PerDeviceOnce attrs;
-    const cudaError_t attr_error = attrs.run([] {
-        cudaError_t e = cudaFuncSetAttribute(prefill_attend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(prefill_attend_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-        return e;
-    });
+    const cudaError_t attr_error = set_attributes();
     if (attr_error != cudaSuccess) return attr_error;
     const int32_t heads_q = l.kv_heads * g;
     CUtensorMap map_q, map_k, map_v;
@@ -674,6 +795,7 @@ cudaError_t launch_prefill(const freqkv_layout& l, const void* k, const void* v,
         job.batch0 = b0;
         job.batch_count = nb;
         PrefillParams prm;
+        prm.unit = nullptr;
         for (int32_t i = 0; i < nb; ++i) {
             job.len[i] = prm.len[i] = lens_host[b0 + i];
             max_len = std::max(max_len, lens_host[b0 + i]);
@@ -704,7 +826,102 @@ cudaError_t launch_prefill(const freqkv_layout& l, const void* k, const void* v,
         attr.val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        e = cudaLaunchKernelEx(&cfg, prefill_attend_kernel, map_q, map_k, map_v, prm);
+        e = cudaLaunchKernelEx(&cfg, prefill_attend_kernel<false>, map_q, map_k, map_v, prm);
+        if (e != cudaSuccess) return e;
+        *kernels_launched += 2;
+    }
+    return cudaSuccess;
+}
+
+size_t prefill_q8_scratch_bytes(const Q8View& cache, int32_t batch, int32_t capacity)
+{
+    return (size_t)batch * cache.kv_heads * capacity * 512 + (size_t)batch * cache.kv_heads * sizeof(float);
+}
+
+cudaError_t launch_prefill_q8(const Q8View& cache, int32_t batch, int32_t capacity, int32_t layer, const void* q, void* out, int32_t g,
+                              int32_t n_new, const int32_t* lens_host, const float2* table, float scale, void* scratch, void* query_scratch,
+                              int32_t* status, unsigned long long wait_limit_ns, const char** error, int32_t* kernels_launched, cudaStream_t stream)
+{
+    *error = nullptr;
+    if (!encode_fn()) {
+        *error = "cuTensorMapEncodeTiled is not available from this driver";
+        return cudaErrorNotSupported;
+    }
+    const cudaError_t attr_error = set_attributes();
+    if (attr_error != cudaSuccess) return attr_error;
+    const int32_t heads_q = cache.kv_heads * g;
+    const int64_t slices = (int64_t)batch * cache.kv_heads, one = slices * capacity * 128;
+    __half* keys = static_cast<__half*>(scratch);
+    __half* vals = keys + one;
+    float* unit = reinterpret_cast<float*>(vals + one);
+    CUtensorMap map_q, map_k, map_v;
+    if (!encode_rows_map(&map_q, query_scratch, n_new, (int64_t)batch * heads_q, BQ) || !encode_rows_map(&map_k, keys, capacity, slices, BKV) ||
+        !encode_rows_map(&map_v, vals, capacity, slices, BKV)) {
+        *error = "cuTensorMapEncodeTiled rejected a tensor of the prefill attention";
+        return cudaErrorInvalidValue;
+    }
+    const int32_t per_launch = std::max(1, std::min(PREFILL_MAX_BATCH, 65535 / (cache.kv_heads + heads_q)));
+    for (int32_t b0 = 0; b0 < batch; b0 += per_launch) {
+        const int32_t nb = std::min(per_launch, batch - b0);
+        int32_t max_len = 0;
+        Q8RopeJob job;
+        const int64_t scale_layer = (int64_t)layer * cache.kv_heads * cache.blocks;
+        job.k = static_cast<const uint8_t*>(cache.codes[0]) + layer * cache.stride_layer;
+        job.v = static_cast<const uint8_t*>(cache.codes[1]) + layer * cache.stride_layer;
+        job.k_scale = cache.scales[0] + scale_layer;
+        job.v_scale = cache.scales[1] + scale_layer;
+        job.stride_batch = cache.stride_batch;
+        job.stride_head = cache.stride_head;
+        job.stride_token = cache.stride_token;
+        job.scale_batch = (int64_t)cache.layers * cache.kv_heads * cache.blocks;
+        job.blocks = cache.blocks;
+        job.block_shift = cache.block_tokens == 16 ? 4 : cache.block_tokens == 32 ? 5 : cache.block_tokens == 64 ? 6 : 7;
+        job.kind = cache.kind;
+        job.q = static_cast<const __nv_bfloat16*>(q);
+        job.k_out = keys;
+        job.v_out = vals;
+        job.unit = unit;
+        job.q_out = static_cast<__half*>(query_scratch);
+        job.table = table;
+        job.qscale = scale * 1.4426950408889634f;
+        job.kv_heads = cache.kv_heads;
+        job.heads_q = heads_q;
+        job.n_new = n_new;
+        job.capacity = capacity;
+        job.batch0 = b0;
+        job.batch_count = nb;
+        PrefillParams prm;
+        for (int32_t i = 0; i < nb; ++i) {
+            job.len[i] = prm.len[i] = lens_host[b0 + i];
+            max_len = std::max(max_len, lens_host[b0 + i]);
+        }
+        job.k_rows = std::min(capacity, (max_len + BKV - 1) / BKV * BKV);
+        const dim3 rope_grid((unsigned)((std::max(job.k_rows, n_new) + 63) / 64), (unsigned)(nb * (cache.kv_heads + heads_q)));
+        prefill_q8_rope_kernel<<<rope_grid, 256, 0, stream>>>(job);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        prm.n_new = n_new;
+        prm.kv_heads = cache.kv_heads;
+        prm.g = g;
+        prm.layer = layer;
+        prm.batch0 = b0;
+        prm.batch_count = nb;
+        prm.q_tiles = (n_new + BQ - 1) / BQ;
+        prm.unit = unit;
+        prm.out = static_cast<__nv_bfloat16*>(out);
+        prm.status = status;
+        prm.wait_limit_ns = wait_limit_ns;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)((int64_t)prm.q_tiles * heads_q * nb));
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = SMEM_BYTES;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;  // let the launch overlap the tail of pass 1
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, prefill_attend_kernel<true>, map_q, map_k, map_v, prm);
         if (e != cudaSuccess) return e;
         *kernels_launched += 2;
     }

@@ -216,3 +216,84 @@ def test_decode_refusals(ctx):
     with pytest.raises(fk.FreqKVError) as e:
         ctx.attend_decode_q8(cache, 0, queries((1, 130, 128), 3), [5])
     assert e.value.status == fk.ERR_UNSUPPORTED
+
+
+# ---- chunks ----
+
+def check_prefill(ctx, cache, layer, q, lens, base=10000.0, scale=0.0, kv=None, heads=None):
+    out = ctx.attend_prefill_q8(cache, layer, q, lens, rope_base=base, scale=scale)
+    assert ctx.last_device_status() == fk.OK
+    k, v = kv if kv is not None else values(cache)
+    B, Hq, n, _ = q.shape
+    G = Hq // k.shape[2]
+    for b, h in heads or [(b, h) for b in range(B) for h in range(Hq)]:
+        tokens = sorted({0, 1, n // 2, n - 1} | {t for t in (63, 64, 127, 128, 129) if t < n})
+        want = [oa.attend_decode(q[b, h:h + 1, t].double().cpu().numpy(), k[b, layer, h // G], v[b, layer, h // G], lens[b] - n + t + 1, base,
+                                 None if scale <= 0 else scale) for t in tokens if t < n]
+        near(out[b, h, [t for t in tokens if t < n]], np.stack(want))
+    return out
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("G,n,lens,block", [(1, 1, [1, 70], 16), (2, 2, [2, 3], 32), (3, 64, [64, 200], 64), (4, 129, [129, 300], 128),
+                                            (1, 200, [230, 299], 16), (9, 5, [65, 128], 64)])
+def test_prefill_small(ctx, kind, G, n, lens, block):
+    cache = make(ctx, 2, 2, 2, 300, kind, block, seed=n, row_pad=16)
+    check_prefill(ctx, cache, 1, queries((2, 2 * G, n, 128), n), lens)
+
+
+@pytest.mark.parametrize("base,scale", [(0.0, 0.0), (500000.0, 0.05)])
+def test_prefill_rope_off_other_base_and_scale(ctx, base, scale):
+    cache = make(ctx, 1, 1, 2, 500, "e4m3", 64, seed=21, spread=0.3)
+    check_prefill(ctx, cache, 0, queries((1, 4, 130, 128), 3), [497], base, scale)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+def test_prefill_scales_of_any_size_and_rows_behind_the_last(ctx, kind):
+    cache = make(ctx, 1, 1, 1, 640, kind, 64, seed=22)
+    for i, e in enumerate((60, 58, 59, None, 60, 57, 60, 55, 60, 60)):
+        cache.v_scale[0, 0, :, i].mul_(0.0 if e is None else 2.0 ** e)
+    kv = values(cache)
+    if kind == "e4m3":
+        for c in (cache.k, cache.v):
+            c.view(torch.int8)[:, :, :, 570:] = 0x7f
+    check_prefill(ctx, cache, 0, queries((1, 2, 300, 128), 3), [570], kv=kv)
+
+
+def test_prefill_of_one_token_is_decoding(ctx):
+    cache = make(ctx, 2, 1, 2, 777, "int8", 32, seed=23)
+    q = queries((2, 8, 128), 4)
+    a, b = ctx.attend_decode_q8(cache, 0, q, [777, 5]), ctx.attend_prefill_q8(cache, 0, q.unsqueeze(2), [777, 5])
+    assert float((a.float() - b.squeeze(2).float()).norm() / a.float().norm()) <= 2 * ALL
+
+
+def test_a_stream_in_8_bits(ctx):
+    """As they are used: chunks are appended and attend, the full cache goes out, is compressed and comes back, tokens are appended
+    and attend.  The attention is compared with the bf16 calls on the same rows, dequantized."""
+    B, L, H, cap, G, sink = 2, 2, 2, 320, 4, 4
+    cache = fk.Q8Cache.empty(B, L, H, cap, kind=fk.Q8_E4M3, block_tokens=32)
+    work = [torch.zeros(B, L, H, cap, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lens, seed = [0, 0], 40
+    for n in (160, 160, None, 100, 1, 1, 56):
+        seed += 1
+        if n is None:                                  # full: e4m3 values are exact in bf16
+            with pytest.raises(fk.FreqKVError) as e:
+                ctx.append_q8(cache, new[0][:, :, :, :1].contiguous(), new[1][:, :, :, :1].contiguous(), lens)
+            assert e.value.status == fk.ERR_CAPACITY
+            ctx.dequantize(cache, lens, *work)
+            kept = (cap - sink) // 2
+            lens = [ctx.compress(*work, cap, kept, sink)] * B
+            ctx.quantize(*work, lens, cache)
+            continue
+        new = [rows((B, L, H, n, 128), torch.bfloat16, seed + 100 * i, 0.3) for i in range(2)]
+        lens = ctx.append_q8(cache, *new, lens)
+        ctx.dequantize(cache, lens, *work)
+        for layer in range(L):
+            q = queries((B, H * G, n, 128), seed + layer)
+            if n == 1:
+                a, b = ctx.attend_decode_q8(cache, layer, q[:, :, 0].contiguous(), lens), ctx.attend_decode(*work, layer, q[:, :, 0].contiguous(), lens)
+            else:
+                a, b = ctx.attend_prefill_q8(cache, layer, q, lens), ctx.attend_prefill(*work, layer, q, lens)
+            assert float((a.float() - b.float()).norm() / b.float().norm()) <= 2 * ALL
+    assert ctx.last_device_status() == fk.OK
+    assert lens == [sink + 158 + 158] * B

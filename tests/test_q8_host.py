@@ -86,6 +86,30 @@ def test_check_quantize():
     assert quantize(src(), lay(), [10], ks=NK) == fk.ERR_INVALID_ARG      # codes over the source
 
 
+def test_check_attend_q8():
+    Q, O = NK, NV
+
+    def check_attend(layout, lens, layer=0, q=Q, out=O, G=1, n_new=1):
+        return fk.lib().freqkv_check_attend_q8(ctypes.byref(layout), K, V, KS, VS, layer, q, out, G, n_new, (ctypes.c_int32 * len(lens))(*lens))
+
+    assert check_attend(lay(B=2), [1, 256]) == fk.OK
+    for G in (1, 3, 8, 9, 64):
+        assert check_attend(lay(), [10], G=G) == fk.OK
+    assert check_attend(lay(), [10], G=65) == fk.ERR_UNSUPPORTED
+    assert check_attend(lay(), [10], G=0) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [0]) == fk.ERR_INVALID_ARG            # an empty cache has nothing to attend to
+    assert check_attend(lay(), [257]) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], layer=2) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], layer=-1) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], q=0) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], out=Q) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], q=Q + 2) == fk.ERR_UNSUPPORTED
+    assert check_attend(lay(hd=64), [10]) == fk.ERR_UNSUPPORTED
+    assert check_attend(lay(), [10], n_new=0) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], n_new=11) == fk.ERR_INVALID_ARG
+    assert check_attend(lay(), [10], n_new=10) == fk.OK
+
+
 def test_null_context_and_binding_checks():
     one = (ctypes.c_int32 * 1)(0)
     lib, layout = fk.lib(), lay()
