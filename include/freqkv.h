@@ -347,6 +347,36 @@ freqkv_status freqkv_attend_prefill_q8(freqkv_ctx* ctx, const freqkv_q8_layout* 
                                        const float* v_scale, int32_t layer, const void* q, void* out, int32_t q_heads_per_kv,
                                        int32_t n_new, const int32_t* lens, float rope_base, float scale, void* cuda_stream);
 
+/* ---- eviction by accumulated attention weight: the other way to shorten a full cache ----
+ *
+ * `mass` is a DEVICE array, dense fp32 [batch, layers, kv_heads, capacity]: what attention weight each cache row has received so far,
+ * summed over the query heads of its KV head and over the tokens that have attended.  The caller starts it at zeros (rows that are
+ * appended later find zeros there); freqkv_attend_decode_mass and freqkv_attend_mass add to it, freqkv_evict reads it, moves it with the rows and
+ * zeroes what it frees.  Sums and weights are fp32 throughout. */
+
+/* freqkv_attend_decode that also adds the softmax weights:  mass[b, layer, h, j] += sum over the q_heads_per_kv query heads of h of
+ * the weight of row j,  j < lens[b].  Other rows and layers of mass keep their values.  Scores, weights and sums are fp32 (bf16 caches with
+ * grouped queries, too).  Everything else, errors included, as for freqkv_attend_decode; mass may not be NULL (INVALID_ARG) and is
+ * 4-byte aligned (UNSUPPORTED).  Results do not depend on the order of atomics: there are none. */
+freqkv_status freqkv_attend_decode_mass(freqkv_ctx* ctx, const freqkv_layout* layout, const void* k, const void* v, int32_t layer,
+                                        const void* q, void* out, float* mass, int32_t q_heads_per_kv, const int32_t* lens,
+                                        float rope_base, float scale, void* cuda_stream);
+
+/* Shortens every sequence of a cache by its lightest rows.  Of the lens[b] rows of sequence b, every (layer, kv_head) keeps the first
+ * `sink`, the last `recent`, and of those between the kept_len[b] - recent with the largest mass (equal masses: the lower row; NaN counts
+ * as larger than any number); K and V keep the same rows.  The kept rows move, in their order, to rows [0, sink + kept_len[b]); keys are cached before
+ * RoPE, so they take the positions of their new rows.  Cache rows from there on keep their bytes.  On success lens[b] = sink + kept_len[b].
+ *   mass       as above; only its rows j < lens[b] are read, between sink and recent ones.
+ *   mass_out   receives the kept rows' masses at their new rows and zeros at rows [new length, old length); may be `mass` itself.
+ *   kept_rows  optional (NULL): dense int32 [batch, layers, kv_heads, capacity]; entries [0, new length) receive the kept rows' old
+ *              indexes.  Without it the context's staging area holds them, which a capture cannot allocate.
+ *   lens, kept_len  HOST arrays of `batch` entries.
+ * Any layout of freqkv_layout's rules, bf16 or fp32.  Errors: INVALID_ARG (null pointers, sink < 0, recent < 0, lens[b] outside [sink,
+ * capacity], kept_len[b] outside [recent, lens[b] - sink], arrays that overlap other than mass_out == mass), UNSUPPORTED (layout rules,
+ * misaligned pointers), ALLOC, CUDA. */
+freqkv_status freqkv_evict(freqkv_ctx* ctx, const freqkv_layout* layout, void* k, void* v, const float* mass, float* mass_out,
+                           int32_t* kept_rows, int32_t* lens, const int32_t* kept_len, int32_t sink, int32_t recent, void* cuda_stream);
+
 /* Instrumentation for benchmarks.  With timing enabled every compression records a CUDA event
  * pair on the caller's stream around its transform kernel (the projection / fast-transform
  * launch, not the copy-back or table builders; the folded fp32 product's three launches together).  freqkv_get_timing waits for the recorded
@@ -432,6 +462,8 @@ freqkv_status freqkv_check_attend_q8(const freqkv_q8_layout* layout, const void*
 freqkv_status freqkv_check_quantize(const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
                                     const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
                                     const float* v_scale);
+freqkv_status freqkv_check_evict(const freqkv_layout* layout, const void* k, const void* v, const float* mass, const float* mass_out,
+                                 const int32_t* kept_rows, const int32_t* lens, const int32_t* kept_len, int32_t sink, int32_t recent);
 
 /* Host-only diagnostic of the fast transform's plan (no device, no context): applies the
  * factored chain the FDCT variant would run for (n_in, n_keep) -- same factor choice, same

@@ -35,6 +35,7 @@ EXPORTS = [
     "freqkv_set_wait_limit", "freqkv_selftest_bounded_wait", "freqkv_fast_plan_apply_host", "freqkv_set_fast_family", "freqkv_gemm_fold_levels", "freqkv_gemm_blocks",
     "freqkv_append_q8", "freqkv_quantize", "freqkv_dequantize", "freqkv_check_append_q8", "freqkv_check_quantize",
     "freqkv_attend_decode_q8", "freqkv_check_attend_q8", "freqkv_attend_prefill_q8",
+    "freqkv_attend_decode_mass", "freqkv_evict", "freqkv_check_evict",
 ]
 NOALLOC_MAX_BASIS_ELEMS = 1 << 20
 NOALLOC_STAGING_BYTES = 4 << 20
@@ -128,6 +129,10 @@ def lib() -> ctypes.CDLL:
         L.freqkv_attend_prefill_q8.argtypes = [c_void_p, QP, *four, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P, ctypes.c_float,
                                                ctypes.c_float, c_void_p]
         L.freqkv_check_attend_q8.argtypes = [QP, *four, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P]
+        L.freqkv_attend_decode_mass.argtypes = [c_void_p, LP, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, I32P,
+                                                ctypes.c_float, ctypes.c_float, c_void_p]
+        L.freqkv_evict.argtypes = [c_void_p, LP, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, I32P, I32P, c_int32, c_int32, c_void_p]
+        L.freqkv_check_evict.argtypes = [LP, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, I32P, I32P, c_int32, c_int32]
         L.freqkv_last_error.argtypes = [c_void_p]
         L.freqkv_last_error.restype = c_char_p
         L.freqkv_status_string.argtypes = [c_int]
@@ -545,6 +550,51 @@ class Context:
         if out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
             raise FreqKVError(ERR_INVALID_ARG, "out must be dense and like q")
         return out
+
+    @staticmethod
+    def _per_row(t: torch.Tensor, k: torch.Tensor, dtype: torch.dtype, what: str):
+        if t.dtype != dtype or tuple(t.shape) != tuple(k.shape[:4]) or not t.is_contiguous() or t.device != k.device:
+            raise FreqKVError(ERR_INVALID_ARG, f"{what} must be dense {dtype} [batch, layers, kv_heads, capacity] on the cache's device")
+
+    def attend_decode_mass(self, k: torch.Tensor, v: torch.Tensor, layer: int, q: torch.Tensor, mass: torch.Tensor, lens: list[int],
+                           rope_base: float = 10000.0, scale: float = 0.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """``attend_decode`` that also adds the softmax weights, summed over the query heads of each KV head, to ``mass``
+        (fp32 [batch, layers, kv_heads, capacity], in place).  Returns ``out``."""
+        lay = layout_of(k)
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise FreqKVError(ERR_INVALID_ARG, "K and V must share shape, strides and dtype")
+        if q.dim() != 3 or not q.is_contiguous() or q.dtype != k.dtype or q.shape[0] != lay.batch or \
+                q.shape[2] != lay.head_dim or q.shape[1] % lay.kv_heads != 0 or len(lens) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "q must be dense [batch, q_heads, head_dim] in the cache dtype, lens one entry per sequence")
+        self._per_row(mass, k, torch.float32, "mass")
+        out = self._out(q, out)
+        st = lib().freqkv_attend_decode_mass(self._h, ctypes.byref(lay), k.data_ptr(), v.data_ptr(), layer, q.data_ptr(), out.data_ptr(),
+                                             mass.data_ptr(), q.shape[1] // lay.kv_heads, (c_int32 * lay.batch)(*lens), rope_base, scale,
+                                             _stream_ptr(stream))
+        self._check(st, "freqkv_attend_decode_mass")
+        return out
+
+    def evict(self, k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, lens: list[int], kept_len: list[int], sink: int, recent: int,
+              mass_out: torch.Tensor | None = None, kept_rows: torch.Tensor | None = None, stream=None) -> list[int]:
+        """Every (sequence, layer, KV head) keeps its first ``sink`` rows, its last ``recent`` ones and the heaviest of the others,
+        ``kept_len[b]`` besides the sinks in all; K, V and mass move up in place (the masses to ``mass_out`` where given).  ``kept_rows``
+        (int32 [batch, layers, kv_heads, capacity]) receives the kept rows' old indexes.  Returns the new lengths."""
+        lay = layout_of(k)
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise FreqKVError(ERR_INVALID_ARG, "K and V must share shape, strides and dtype")
+        if len(lens) != lay.batch or len(kept_len) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "lens and kept_len need one entry per sequence")
+        mass_out = mass if mass_out is None else mass_out
+        self._per_row(mass, k, torch.float32, "mass")
+        self._per_row(mass_out, k, torch.float32, "mass_out")
+        if kept_rows is not None:
+            self._per_row(kept_rows, k, torch.int32, "kept_rows")
+        c_lens = (c_int32 * lay.batch)(*lens)
+        st = lib().freqkv_evict(self._h, ctypes.byref(lay), k.data_ptr(), v.data_ptr(), mass.data_ptr(), mass_out.data_ptr(),
+                                kept_rows.data_ptr() if kept_rows is not None else None, c_lens, (c_int32 * lay.batch)(*kept_len), sink,
+                                recent, _stream_ptr(stream))
+        self._check(st, "freqkv_evict")
+        return list(c_lens)
 
     def compress_host(self, k_host: torch.Tensor, v_host: torch.Tensor, cache_len: int, kept_len: int, sink: int,
                       stream=None) -> tuple[int, int, int]:

@@ -213,13 +213,21 @@ freqkv_status prefill_scratch(freqkv_ctx* ctx, size_t key_bytes, size_t query_by
     return FREQKV_OK;
 }
 
-}  // namespace freqkv
-
-namespace {
-
-constexpr size_t kScratchChunkBytes = size_t(1) << 30;  // per-chunk output staging of the scratch paths
-constexpr int32_t kDctRows = -1;  // plan key of the plain DCT matrix (power spectrum) among the retained-band offsets
-constexpr size_t kBasisBudgetBytes = size_t(12) << 30;  // plan cache is flushed beyond this
+freqkv_status get_scratch(freqkv_ctx* ctx, size_t bytes, void** out)
+{
+    if (bytes > ctx->scratch_bytes) {
+        if (ctx->scratch) {
+            FREQKV_CUDA(ctx, cudaDeviceSynchronize());  // earlier launches may still read it
+            cudaFree(ctx->scratch);
+            ctx->scratch = nullptr;
+            ctx->scratch_bytes = 0;
+        }
+        FREQKV_CUDA(ctx, cudaMalloc(&ctx->scratch, bytes));
+        ctx->scratch_bytes = bytes;
+    }
+    *out = ctx->scratch;
+    return FREQKV_OK;
+}
 
 CacheView make_view(const freqkv_layout& l, void* k, void* v, int32_t batch0, int32_t batch_count)
 {
@@ -237,6 +245,20 @@ CacheView make_view(const freqkv_layout& l, void* k, void* v, int32_t batch0, in
     w.batch0 = batch0;
     return w;
 }
+
+bool apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
+{
+    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+    return x + a_bytes <= y || y + b_bytes <= x;
+}
+
+}  // namespace freqkv
+
+namespace {
+
+constexpr size_t kScratchChunkBytes = size_t(1) << 30;  // per-chunk output staging of the scratch paths
+constexpr int32_t kDctRows = -1;  // plan key of the plain DCT matrix (power spectrum) among the retained-band offsets
+constexpr size_t kBasisBudgetBytes = size_t(12) << 30;  // plan cache is flushed beyond this
 
 bool is_pow2(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
 
@@ -485,22 +507,6 @@ void free_basis(Basis* b)
     if (b->f32_fold) cudaFree(b->f32_fold);
     if (b->nearfar) cudaFree(b->nearfar);
     *b = Basis();
-}
-
-freqkv_status get_scratch(freqkv_ctx* ctx, size_t bytes, void** out)
-{
-    if (bytes > ctx->scratch_bytes) {
-        if (ctx->scratch) {
-            FREQKV_CUDA(ctx, cudaDeviceSynchronize());  // earlier launches may still read it
-            cudaFree(ctx->scratch);
-            ctx->scratch = nullptr;
-            ctx->scratch_bytes = 0;
-        }
-        FREQKV_CUDA(ctx, cudaMalloc(&ctx->scratch, bytes));
-        ctx->scratch_bytes = bytes;
-    }
-    *out = ctx->scratch;
-    return FREQKV_OK;
 }
 
 // Compress `count` sequences starting at batch0, all with the same (n_in, n_keep).  `of_triples`: the triples of the whole call where

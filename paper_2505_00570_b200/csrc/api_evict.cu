@@ -1,0 +1,116 @@
+// C ABI of eviction by accumulated attention weight: argument validation and dispatch.
+#include <algorithm>
+#include <cmath>
+
+#include "ctx.cuh"
+#include "evict.cuh"
+
+using namespace freqkv;
+
+namespace {
+
+int64_t mass_bytes(const freqkv_layout& l) { return (int64_t)l.batch * l.layers * l.kv_heads * l.capacity * (int64_t)sizeof(float); }
+
+freqkv_status check_mass(const float* mass)
+{
+    if (!mass) return FREQKV_ERR_INVALID_ARG;
+    return (uintptr_t)mass & 3 ? FREQKV_ERR_UNSUPPORTED : FREQKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+freqkv_status freqkv_attend_decode_mass(freqkv_ctx* ctx, const freqkv_layout* layout, const void* k, const void* v, int32_t layer,
+                                        const void* q, void* out, float* mass, int32_t q_heads_per_kv, const int32_t* lens,
+                                        float rope_base, float scale, void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    freqkv_status st = freqkv_check_attend(layout, k, v, layer, q, out, q_heads_per_kv, lens);
+    if (st != FREQKV_OK) return st;
+    st = check_mass(mass);
+    if (st != FREQKV_OK) return st;
+    if (!(scale == scale) || !(rope_base == rope_base)) return FREQKV_ERR_INVALID_ARG;  // NaN
+    const freqkv_layout& l = *layout;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    WorkOrder order(ctx, stream);
+    if (scale <= 0.f) scale = 1.0f / sqrtf((float)l.head_dim);
+    const float2* table = nullptr;
+    const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
+    if (ts != FREQKV_OK) return ts;
+    AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads, attend_resident(q_heads_per_kv, FREQKV_F32, ctx->sm_count), lens);
+    plan.captured = is_capturing(stream);
+    plan.one_wave = false;  // no tickets: a second kernel follows anyway
+    AttendWork work;
+    const int32_t heads = l.kv_heads * q_heads_per_kv;
+    const freqkv_status ws = attend_work_for(ctx, plan, l.batch, heads, l.capacity,
+                                             attend_score_bytes(l.batch, heads, l.capacity), stream, &work);
+    if (ws != FREQKV_OK) return ws;
+    int32_t launched = 0;
+    cudaError_t e;
+    {
+        TransformTimer timer(ctx, stream);
+        e = launch_attend_mass(l, k, v, layer, q, out, mass, q_heads_per_kv, lens, table, scale, plan, work.partial,
+                               reinterpret_cast<float*>(work.more), &launched, stream);
+    }
+    ctx->kernels_launched += launched;
+    return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "attend_decode_mass");
+}
+
+freqkv_status freqkv_check_evict(const freqkv_layout* layout, const void* k, const void* v, const float* mass, const float* mass_out,
+                                 const int32_t* kept_rows, const int32_t* lens, const int32_t* kept_len, int32_t sink, int32_t recent)
+{
+    if (!lens || !kept_len) return FREQKV_ERR_INVALID_ARG;
+    freqkv_status st = check_layout(layout);
+    if (st != FREQKV_OK) return st;
+    st = check_tensors(*layout, k, v);
+    if (st != FREQKV_OK) return st;
+    for (const float* m : {mass, mass_out}) {
+        st = check_mass(m);
+        if (st != FREQKV_OK) return st;
+    }
+    if ((uintptr_t)kept_rows & 3) return FREQKV_ERR_UNSUPPORTED;
+    const int64_t rows = span_elements(*layout) * (int64_t)dtype_size(layout->dtype), m = mass_bytes(*layout);
+    if (mass != mass_out && !apart(mass, m, mass_out, m)) return FREQKV_ERR_INVALID_ARG;
+    for (const void* x : {k, v})
+        if (!apart(x, rows, mass, m) || !apart(x, rows, mass_out, m) || (kept_rows && !apart(x, rows, kept_rows, m))) return FREQKV_ERR_INVALID_ARG;
+    if (kept_rows && (!apart(kept_rows, m, mass, m) || !apart(kept_rows, m, mass_out, m))) return FREQKV_ERR_INVALID_ARG;
+    if (sink < 0 || recent < 0) return FREQKV_ERR_INVALID_ARG;
+    for (int32_t b = 0; b < layout->batch; ++b)
+        if (lens[b] < sink || lens[b] > layout->capacity || kept_len[b] < recent || kept_len[b] > lens[b] - sink) return FREQKV_ERR_INVALID_ARG;
+    return FREQKV_OK;
+}
+
+freqkv_status freqkv_evict(freqkv_ctx* ctx, const freqkv_layout* layout, void* k, void* v, const float* mass, float* mass_out,
+                           int32_t* kept_rows, int32_t* lens, const int32_t* kept_len, int32_t sink, int32_t recent, void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_evict(layout, k, v, mass, mass_out, kept_rows, lens, kept_len, sink, recent);
+    if (st != FREQKV_OK) return st;
+    const freqkv_layout& l = *layout;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    WorkOrder order(ctx, stream);
+    int32_t* rows = kept_rows;
+    int64_t stride = l.capacity;
+    if (!rows) {
+        stride = std::max(1, sink + *std::max_element(kept_len, kept_len + l.batch));
+        void* area = nullptr;
+        const freqkv_status ss = get_scratch(ctx, (size_t)l.batch * l.layers * l.kv_heads * stride * sizeof(int32_t), &area);
+        if (ss != FREQKV_OK) return ss;
+        rows = static_cast<int32_t*>(area);
+    }
+    const CacheView view = make_view(l, k, v, 0, l.batch);
+    int32_t launched = 0;
+    const cudaError_t e = launch_evict(view, l.dtype, l.batch, l.capacity, mass, mass_out, rows, stride, lens, kept_len, sink, recent,
+                                       ctx->sm_count, &launched, stream);
+    ctx->kernels_launched += launched;
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "evict");
+    for (int32_t b = 0; b < l.batch; ++b) lens[b] = sink + kept_len[b];
+    return FREQKV_OK;
+}
+
+}  // extern "C"

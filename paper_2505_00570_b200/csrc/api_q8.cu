@@ -28,12 +28,6 @@ freqkv_status check_q8_layout(const freqkv_q8_layout* l)
     return FREQKV_OK;
 }
 
-bool apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
-{
-    const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
-    return x + a_bytes <= y || y + b_bytes <= x;
-}
-
 int64_t q8_span(const freqkv_q8_layout& l)
 {
     return (int64_t)(l.batch - 1) * l.stride_batch + (int64_t)(l.layers - 1) * l.stride_layer + (int64_t)(l.kv_heads - 1) * l.stride_head +

@@ -42,6 +42,8 @@ struct AttendParams {
     int32_t* tickets;        // [batch * kv_heads]: splits finished so far, 0 between launches; null: attend_merge_kernel follows
     const float2* table;     // [rows][64]: cos, sin of row * base^(-2c/128); null = no RoPE
     float qscale;            // scale * log2(e)
+    float* scores;           // MASS: [batch][kv_heads * G][score_rows], in units of log2
+    int64_t score_rows;
     int32_t total_batch;
     int32_t len[ATTEND_MAX_BATCH];
     uint16_t tiles[ATTEND_MAX_BATCH];  // of 16 rows in one split of each sequence
@@ -180,7 +182,8 @@ __device__ __forceinline__ void merge_splits(const AttendParams& p, int32_t b, i
 
 // TICKETS: the last CTA of a group merges its splits (AttendParams::tickets); else attend_merge_kernel follows.  (As a branch
 // of one kernel the merge cost the calls that do not use it 1 %.)
-template <typename T, int G, bool TICKETS>
+// MASS: the scores are written down and the maximum and sum of every split, too; mass_finish_kernel follows.
+template <typename T, int G, bool TICKETS, bool MASS = false>
 __global__ void __launch_bounds__(THREADS, (G <= 4 ? 2 : 1)) attend_partial_kernel(const AttendParams p)
 {
     wait_for_previous_grid();
@@ -296,6 +299,9 @@ __global__ void __launch_bounds__(THREADS, (G <= 4 ? 2 : 1)) attend_partial_kern
             for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
                 for (int off = 8; off >= 1; off >>= 1) s[g][r] += __shfl_xor_sync(0xffffffffu, s[g][r], off);
+                if constexpr (MASS)
+                    if (l16 == g * ROWS + r && j + r < j1)
+                        p.scores[(((int64_t)(p.batch0 + b) * p.kv_heads + h) * G + g) * p.score_rows + j + r] = s[g][r];
                 if (j + r >= j1) s[g][r] = NEG;
             }
             float mn = m[g];
@@ -357,7 +363,7 @@ __global__ void __launch_bounds__(THREADS, (G <= 4 ? 2 : 1)) attend_partial_kern
             sum = fmaf(sm_ml[w][g][1], f, sum);
             acc = fmaf(sm_o[w][g][c], f, acc);
         }
-        if (n_splits == 1) {
+        if (!MASS && n_splits == 1) {
             store1(static_cast<T*>(p.out) + (((int64_t)(p.batch0 + b) * p.kv_heads + h) * G + g) * 128 + c, acc / sum);
             continue;
         }
@@ -678,6 +684,70 @@ __global__ void __launch_bounds__(128) attend_merge_kernel(const MergeParams p)
     store1(static_cast<T*>(p.out) + head * 128 + c, acc / sum);
 }
 
+// What follows the splits of attend_partial_kernel<MASS>: every block merges the maxima and sums of its heads' splits; then blocks
+// x < gridDim.x - 1 turn MASS_ROWS scores of each head into weights and add them to the rows' mass, the last one merges the outputs.
+struct MassParams {
+    const float* partial;
+    const float* scores;
+    int64_t score_rows;
+    void* out;
+    float* mass;             // moved to the layer: [batch][mass_batch]: [kv_heads][mass_rows]
+    int64_t mass_batch, mass_rows;
+    int32_t kv_heads, batch0, total_batch;
+    int32_t len[ATTEND_MAX_BATCH];
+    uint16_t splits[ATTEND_MAX_BATCH];
+};
+constexpr int MASS_THREADS = 128, MASS_ROWS = 512;
+
+template <typename T, int G>
+__global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_constant__ MassParams p)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float sm_m[G], sm_inv[G];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int32_t b = (int32_t)blockIdx.y / p.kv_heads, h = (int32_t)blockIdx.y % p.kv_heads, splits = p.splits[b], len = p.len[b];
+    const bool merges = blockIdx.x == gridDim.x - 1;
+    const int32_t j0 = (int32_t)blockIdx.x * MASS_ROWS;
+    if (!merges && j0 >= len) return;
+    const int64_t heads_total = (int64_t)p.total_batch * p.kv_heads * G, head0 = ((int64_t)(p.batch0 + b) * p.kv_heads + h) * G;
+    for (int g = warp; g < G; g += MASS_THREADS / 32) {
+        const float* base = p.partial + (head0 + g) * PART;
+        float mx = NEG, sum = 0.f;
+        for (int s = lane; s < splits; s += 32) mx = fmaxf(mx, base[s * heads_total * PART]);
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+        for (int s = lane; s < splits; s += 32) sum = fmaf(base[s * heads_total * PART + 1], ex2(base[s * heads_total * PART] - mx), sum);
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (lane == 0) {
+            sm_m[g] = mx;
+            sm_inv[g] = 1.f / sum;
+        }
+    }
+    __syncthreads();
+    if (merges) {
+        for (int g = 0; g < G; ++g) {
+            float acc = 0.f;
+            for (int s = 0; s < splits; ++s) {
+                const float* pp = p.partial + (s * heads_total + head0 + g) * PART;
+                acc = fmaf(pp[4 + tid], ex2(pp[0] - sm_m[g]), acc);
+            }
+            store1(static_cast<T*>(p.out) + (head0 + g) * 128 + tid, acc * sm_inv[g]);
+        }
+        return;
+    }
+    float* mass = p.mass + (int64_t)(p.batch0 + b) * p.mass_batch + h * p.mass_rows;
+#pragma unroll
+    for (int i = 0; i < MASS_ROWS / MASS_THREADS; ++i) {
+        const int32_t j = j0 + i * MASS_THREADS + tid;
+        if (j >= len) break;
+        float w = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) w = fmaf(ex2(p.scores[(head0 + g) * p.score_rows + j] - sm_m[g]), sm_inv[g], w);
+        mass[j] += w;
+    }
+}
+
 // cos / sin of pos * base^(-2c/128) in fp64, rounded once.
 __global__ void rope_table_kernel(float2* table, int32_t rows, double base)
 {
@@ -735,6 +805,25 @@ cudaError_t launch_mma(const AttendParams& prm, int32_t g, int32_t nb, int32_t s
         default: return cudaErrorInvalidValue;
     }
     return cudaGetLastError();
+}
+
+template <typename T, int G>
+cudaError_t launch_mass_typed(const AttendParams& prm, const MassParams& fin, int32_t nb, int32_t splits, int32_t longest, bool overlap,
+                              cudaStream_t stream)
+{
+    launch_attention(attend_partial_kernel<T, G, false, true>, dim3((unsigned)splits, (unsigned)(nb * prm.kv_heads)), THREADS, 0, stream, prm, overlap);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((longest + MASS_ROWS - 1) / MASS_ROWS + 1), (unsigned)(nb * prm.kv_heads));
+    cfg.blockDim = dim3(MASS_THREADS);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mass_finish_kernel<T, G>, fin);
 }
 
 template <typename T>
@@ -879,6 +968,76 @@ cudaError_t launch_attend(const freqkv_layout& l, const void* k, const void* v, 
             if (me != cudaSuccess) return me;
             ++*launched;
         }
+    }
+    return cudaSuccess;
+}
+
+size_t attend_score_bytes(int32_t batch, int32_t q_heads, int32_t capacity)
+{
+    return (size_t)batch * q_heads * ((capacity + 31) & ~31) * sizeof(float);
+}
+
+cudaError_t launch_attend_mass(const freqkv_layout& l, const void* k, const void* v, int32_t layer, const void* q, void* out, float* mass,
+                               int32_t g, const int32_t* lens_host, const float2* table, float scale, const AttendPlan& plan,
+                               float* partial, float* scores, int32_t* launched, cudaStream_t stream)
+{
+    *launched = 0;
+    const size_t elt = dtype_size(l.dtype);
+    AttendParams prm;
+    prm.k = static_cast<const char*>(k) + (size_t)layer * l.stride_layer * elt;
+    prm.v = static_cast<const char*>(v) + (size_t)layer * l.stride_layer * elt;
+    prm.stride_batch = l.stride_batch;
+    prm.stride_head = l.stride_head;
+    prm.stride_token = l.stride_token;
+    prm.kv_heads = l.kv_heads;
+    prm.q = q;
+    prm.out = out;
+    prm.partial = partial;
+    prm.tickets = nullptr;
+    prm.table = table;
+    prm.qscale = scale * 1.4426950408889634f;
+    prm.scores = scores;
+    prm.total_batch = l.batch;
+    MassParams fin;
+    fin.partial = partial;
+    fin.scores = scores;
+    fin.out = out;
+    fin.mass_rows = l.capacity;
+    fin.mass_batch = (int64_t)l.layers * l.kv_heads * l.capacity;
+    fin.mass = mass + (int64_t)layer * l.kv_heads * l.capacity;
+    fin.kv_heads = l.kv_heads;
+    fin.total_batch = l.batch;
+    prm.score_rows = fin.score_rows = (*std::max_element(lens_host, lens_host + l.batch) + 31) & ~31;
+    const int32_t per_launch = std::max(1, std::min(ATTEND_MAX_BATCH, 65535 / l.kv_heads));
+    for (int32_t b0 = 0; b0 < l.batch; b0 += per_launch) {
+        const int32_t nb = std::min(per_launch, l.batch - b0);
+        prm.batch0 = fin.batch0 = b0;
+        int32_t splits = 1, longest = 1;
+        for (int32_t i = 0; i < nb; ++i) {
+            const int32_t len = lens_host[b0 + i], n = (len + plan.chunk - 1) / plan.chunk, tiles = ((len + n - 1) / n + 15) / 16;
+            prm.len[i] = fin.len[i] = len;
+            prm.tiles[i] = (uint16_t)tiles;
+            fin.splits[i] = (uint16_t)((len + tiles * 16 - 1) / (tiles * 16));
+            splits = std::max(splits, n);
+            longest = std::max(longest, len);
+        }
+        cudaError_t e = cudaErrorInvalidValue;
+        auto run = [&](auto t) {
+            using T = decltype(t);
+            switch (g) {
+                case 1: e = launch_mass_typed<T, 1>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
+                case 2: e = launch_mass_typed<T, 2>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
+                case 4: e = launch_mass_typed<T, 4>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
+                case 8: e = launch_mass_typed<T, 8>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
+                default: break;
+            }
+        };
+        if (l.dtype == FREQKV_F32)
+            run(float());
+        else
+            run(__nv_bfloat16());
+        if (e != cudaSuccess) return e;
+        *launched += 2;
     }
     return cudaSuccess;
 }

@@ -96,6 +96,10 @@ bool is_capturing(cudaStream_t stream);
 freqkv_status check_layout(const freqkv_layout* l);
 freqkv_status check_tensors(const freqkv_layout& l, const void* k, const void* v);
 int64_t span_elements(const freqkv_layout& l);
+bool apart(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes);
+CacheView make_view(const freqkv_layout& l, void* k, void* v, int32_t batch0, int32_t batch_count);
+// The context's staging area, of `bytes` at least.
+freqkv_status get_scratch(freqkv_ctx* ctx, size_t bytes, void** out);
 // The context's cos/sin table of `rope_base`, of `capacity` rows at least; *table stays null when RoPE is off.
 freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base, cudaStream_t stream, const float2** table);
 

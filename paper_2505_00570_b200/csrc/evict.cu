@@ -1,0 +1,237 @@
+// Eviction by accumulated attention weight.
+//
+// Every (batch, layer, kv_head) has its own rows to keep, K and V the same ones: the sinks, the recent rows and the heaviest of the
+// rows between.  Two kernels:
+//
+// evict_select_kernel, a CTA for each triple: the weight of the last row that stays is found digit by digit (three
+// histograms of 11, 11 and 10 bits over the weights as ordered integers; the rows are read again for each, from L2), then one
+// scan over the rows gives every kept row its new place, in order; equal weights at the border go to the lowest rows.  The
+// weights move in the same scan, the old indexes are written down for the second kernel and, if asked for, the caller.
+//
+// evict_move_kernel, a CTA for each matrix (of K and of V) and slice of its channels, moves the rows in place.  A row never moves
+// up, so chunks of rows in ascending order only need their reads to come before their writes: read 128 rows, barrier, write.
+// Bound by memory: the kept rows read and written once (rows that stay where they are are not touched).
+#include <algorithm>
+
+#include "evict.cuh"
+
+namespace freqkv {
+namespace {
+
+constexpr int SELECT_THREADS = 512, SELECT_WARPS = SELECT_THREADS / 32;
+constexpr int BINS = 2048;
+constexpr int MOVE_THREADS = 256, MOVE_UNROLL = 8;
+
+struct SelectParams {
+    const float* mass;
+    float* mass_out;
+    int32_t* rows;
+    int64_t rows_stride;
+    int32_t layers, kv_heads, capacity, batch0, sink, recent;
+    int32_t len[EVICT_MAX_BATCH], kept[EVICT_MAX_BATCH];
+};
+
+// Weights as integers of the same order: NaN above everything, both zeros equal.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    if (x != x) return 0xffffffffu;
+    const uint32_t u = __float_as_uint(x + 0.f);  // -0 + 0 = 0
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __grid_constant__ SelectParams p)
+{
+    __shared__ uint32_t hist[BINS];
+    __shared__ uint2 warp_sum[SELECT_WARPS];
+    __shared__ uint32_t found[2];  // digit; rows above it
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int32_t per_seq = p.layers * p.kv_heads, b = (int32_t)(blockIdx.x / (uint32_t)per_seq);
+    const int64_t triple = (int64_t)p.batch0 * per_seq + blockIdx.x;
+    const int32_t len = p.len[b], kept = p.kept[b], new_len = p.sink + kept;
+    const float* mass = p.mass + triple * p.capacity;
+    float* mass_out = p.mass_out + triple * p.capacity;
+    int32_t* rows = p.rows + triple * p.rows_stride;
+    const int32_t lo = p.sink, hi = len - p.recent, heavy = kept - p.recent;  // 0 <= heavy <= hi - lo
+
+    // the heavy-th largest of rows [lo, hi): its value, and how many of its equals stay
+    uint32_t border = 0xffffffffu, equals = 0;
+    if (heavy > 0) {
+        uint32_t prefix = 0, want = (uint32_t)heavy;  // of the rows that share the digits so far
+        const int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
+#pragma unroll
+        for (int d = 0; d < 3; ++d) {
+            for (int i = tid; i < BINS; i += SELECT_THREADS) hist[i] = 0;
+            __syncthreads();
+            const uint32_t mask = (1u << widths[d]) - 1u;
+            for (int32_t j = lo + tid; j < hi; j += SELECT_THREADS) {
+                const uint32_t key = ordered(mass[j]);
+                if (d == 0 || key >> (shifts[d] + widths[d]) == prefix) atomicAdd(&hist[key >> shifts[d] & mask], 1u);
+            }
+            __syncthreads();
+            // thread t has bins BINS - 4 t - 4 .. + 3; how many rows lie above them
+            uint32_t c[4], mine = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine += c[i] = hist[BINS - 1 - 4 * tid - i];  // descending
+            uint32_t above = mine;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const uint32_t o = __shfl_up_sync(0xffffffffu, above, off);
+                if (lane >= off) above += o;
+            }
+            if (lane == 31) warp_sum[warp].x = above;
+            __syncthreads();
+            for (int w = 0; w < warp; ++w) above += warp_sum[w].x;
+            above -= mine;
+            if (above < want && want <= above + mine) {  // one thread
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (above < want && want <= above + c[i]) {
+                        found[0] = (uint32_t)(BINS - 1 - 4 * tid - i);
+                        found[1] = above;
+                        break;
+                    }
+                    above += c[i];
+                }
+            }
+            __syncthreads();
+            prefix = prefix << widths[d] | found[0];
+            want -= found[1];
+            __syncthreads();
+        }
+        border = prefix;
+        equals = want;
+    }
+    // places: forced rows and rows above the border count, and the first `equals` rows at it
+    uint32_t base_x = 0, base_y = 0;  // so far: rows that stay whatever the border's equals do; rows at the border
+    for (int32_t j0 = 0; j0 < len; j0 += SELECT_THREADS) {
+        const int32_t j = j0 + tid;
+        float m = 0.f;
+        uint32_t sure = 0, equal = 0;
+        if (j < len) {
+            m = mass[j];
+            if (j < lo || j >= hi) {
+                sure = 1;
+            } else if (heavy > 0) {
+                const uint32_t key = ordered(m);
+                sure = key > border;
+                equal = key == border;
+            }
+        }
+        const uint32_t sure_bits = __ballot_sync(0xffffffffu, sure), equal_bits = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1u;
+        if (lane == 0) warp_sum[warp] = make_uint2(__popc(sure_bits), __popc(equal_bits));
+        __syncthreads();  // every thread has read its weight, too: mass_out may be mass
+        uint32_t x = base_x + __popc(sure_bits & below), y = base_y + __popc(equal_bits & below);
+        for (int w = 0; w < SELECT_WARPS; ++w) {
+            const uint2 s = warp_sum[w];
+            if (w < warp) {
+                x += s.x;
+                y += s.y;
+            }
+            base_x += s.x;
+            base_y += s.y;
+        }
+        if (sure || (equal && y < equals)) {
+            const uint32_t at = x + min(y, equals);
+            rows[at] = j;
+            mass_out[at] = m;
+        }
+        __syncthreads();
+    }
+    for (int32_t j = new_len + tid; j < len; j += SELECT_THREADS) mass_out[j] = 0.f;
+}
+
+struct MoveParams {
+    CacheView view;
+    const int32_t* rows;
+    int64_t rows_stride;
+    int32_t batch0, sink, elt, slices, lanes;  // 16-byte lanes a row's slice
+    int32_t kept[EVICT_MAX_BATCH];
+};
+
+__global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const __grid_constant__ MoveParams p)
+{
+    const int32_t slice = (int32_t)(blockIdx.x % (uint32_t)p.slices);
+    const int64_t mat = blockIdx.x / (uint32_t)p.slices;
+    const int tensor = (int)(mat & 1);
+    const int32_t triple = (int32_t)(mat >> 1), per_seq = p.view.layers * p.view.kv_heads, b = triple / per_seq;
+    const int32_t h = triple % p.view.kv_heads, l = triple / p.view.kv_heads % p.view.layers;
+    const int32_t new_len = p.sink + p.kept[b];
+    const int32_t* rows = p.rows + ((int64_t)p.batch0 * per_seq + triple) * p.rows_stride;
+    const int64_t pitch = p.view.stride_token * p.elt;
+    const int32_t lane = threadIdx.x % p.lanes, row_in = threadIdx.x / p.lanes, per_pass = MOVE_THREADS / p.lanes;
+    const int32_t chunk = per_pass * MOVE_UNROLL;
+    const int32_t row_bytes = p.view.head_dim * p.elt, at = (slice * p.lanes + lane) * 16;
+    const bool live = row_in < per_pass && at < row_bytes;
+    char* base = static_cast<char*>(tensor_base(p.view, tensor)) +
+                 ((int64_t)(p.batch0 + b) * p.view.stride_batch + (int64_t)l * p.view.stride_layer + (int64_t)h * p.view.stride_head) * p.elt + at;
+    // the sinks stay where they are
+    for (int32_t d0 = p.sink; d0 < new_len; d0 += chunk) {
+        uint4 v[MOVE_UNROLL];
+        bool moved[MOVE_UNROLL];
+#pragma unroll
+        for (int i = 0; i < MOVE_UNROLL; ++i) {
+            const int32_t d = d0 + i * per_pass + row_in;
+            moved[i] = false;
+            if (live && d < new_len) {
+                const int32_t s = rows[d];
+                moved[i] = s != d;
+                if (moved[i]) v[i] = *reinterpret_cast<const uint4*>(base + s * pitch);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MOVE_UNROLL; ++i)
+            if (moved[i]) *reinterpret_cast<uint4*>(base + (int64_t)(d0 + i * per_pass + row_in) * pitch) = v[i];
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_evict(const CacheView& view, int32_t dtype, int32_t batch, int32_t capacity, const float* mass, float* mass_out,
+                         int32_t* rows, int64_t rows_stride, const int32_t* lens, const int32_t* kept, int32_t sink, int32_t recent,
+                         int sm_count, int32_t* launched, cudaStream_t stream)
+{
+    *launched = 0;
+    SelectParams sel;
+    sel.mass = mass;
+    sel.mass_out = mass_out;
+    sel.rows = rows;
+    sel.rows_stride = rows_stride;
+    sel.layers = view.layers;
+    sel.kv_heads = view.kv_heads;
+    sel.capacity = capacity;
+    sel.sink = sink;
+    sel.recent = recent;
+    MoveParams mov;
+    mov.view = view;
+    mov.rows = rows;
+    mov.rows_stride = rows_stride;
+    mov.sink = sink;
+    mov.elt = (int32_t)dtype_size(dtype);
+    const int32_t row_lanes = view.head_dim * mov.elt / 16;
+    for (int32_t b0 = 0; b0 < batch; b0 += EVICT_MAX_BATCH) {
+        const int32_t nb = std::min(EVICT_MAX_BATCH, batch - b0);
+        sel.batch0 = mov.batch0 = b0;
+        for (int32_t i = 0; i < nb; ++i) {
+            sel.len[i] = lens[b0 + i];
+            sel.kept[i] = mov.kept[i] = kept[b0 + i];
+        }
+        const int64_t triples = (int64_t)nb * view.layers * view.kv_heads;
+        // few matrices: slices of down to 64 bytes of their rows, so that there are CTAs enough for the chip
+        mov.slices = 1;
+        while (mov.slices * 8 <= row_lanes && 2 * triples * mov.slices < (int64_t)sm_count * 4) mov.slices *= 2;
+        mov.lanes = (row_lanes + mov.slices - 1) / mov.slices;
+        if (2 * triples * mov.slices > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        evict_select_kernel<<<(unsigned)triples, SELECT_THREADS, 0, stream>>>(sel);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launched;
+        evict_move_kernel<<<(unsigned)(2 * triples * mov.slices), MOVE_THREADS, 0, stream>>>(mov);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        ++*launched;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace freqkv
