@@ -362,6 +362,18 @@ freqkv_status freqkv_attend_decode_mass(freqkv_ctx* ctx, const freqkv_layout* la
                                         const void* q, void* out, float* mass, int32_t q_heads_per_kv, const int32_t* lens,
                                         float rope_base, float scale, void* cuda_stream);
 
+/* The weights of a chunk of n_new tokens per sequence, whose keys are cache rows [lens[b] - n_new, lens[b]) already (as for
+ * freqkv_attend_prefill, which computes their attention):  mass[b, layer, h, j] += sum over the chunk's tokens i that see row j
+ * (j <= lens[b] - n_new + i) and over the query heads of h of the softmax weight of row j.  q is the chunk's queries,
+ * dense [batch, kv_heads * q_heads_per_kv, n_new, head_dim], bf16; only the last tokens of a prompt may be given (n_new of them).
+ * Scores are products of two fp16 parts of each factor (22 bits) with fp32 sums, weights and their sums fp32; turned keys and queries must stay
+ * below 65504.  bf16 caches with head_dim 128, q_heads_per_kv from 1 to 64.  Work areas and capture as for freqkv_attend_prefill (they are the same
+ * areas).  A wait that runs out shows up in freqkv_last_device_status as TIMEOUT.  Errors: those of freqkv_attend_prefill; mass as for
+ * freqkv_attend_decode_mass. */
+freqkv_status freqkv_attend_mass(freqkv_ctx* ctx, const freqkv_layout* layout, const void* k, int32_t layer, const void* q, float* mass,
+                                 int32_t q_heads_per_kv, int32_t n_new, const int32_t* lens, float rope_base, float scale,
+                                 void* cuda_stream);
+
 /* Shortens every sequence of a cache by its lightest rows.  Of the lens[b] rows of sequence b, every (layer, kv_head) keeps the first
  * `sink`, the last `recent`, and of those between the kept_len[b] - recent with the largest mass (equal masses: the lower row; NaN counts
  * as larger than any number); K and V keep the same rows.  The kept rows move, in their order, to rows [0, sink + kept_len[b]); keys are cached before
@@ -462,6 +474,8 @@ freqkv_status freqkv_check_attend_q8(const freqkv_q8_layout* layout, const void*
 freqkv_status freqkv_check_quantize(const freqkv_layout* src, const void* k_src, const void* v_src, const int32_t* lens,
                                     const freqkv_q8_layout* layout, const void* k, const void* v, const float* k_scale,
                                     const float* v_scale);
+freqkv_status freqkv_check_attend_mass(const freqkv_layout* layout, const void* k, int32_t layer, const void* q, const float* mass,
+                                       int32_t q_heads_per_kv, int32_t n_new, const int32_t* lens);
 freqkv_status freqkv_check_evict(const freqkv_layout* layout, const void* k, const void* v, const float* mass, const float* mass_out,
                                  const int32_t* kept_rows, const int32_t* lens, const int32_t* kept_len, int32_t sink, int32_t recent);
 

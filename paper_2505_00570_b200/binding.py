@@ -36,6 +36,7 @@ EXPORTS = [
     "freqkv_append_q8", "freqkv_quantize", "freqkv_dequantize", "freqkv_check_append_q8", "freqkv_check_quantize",
     "freqkv_attend_decode_q8", "freqkv_check_attend_q8", "freqkv_attend_prefill_q8",
     "freqkv_attend_decode_mass", "freqkv_evict", "freqkv_check_evict",
+    "freqkv_attend_mass", "freqkv_check_attend_mass",
 ]
 NOALLOC_MAX_BASIS_ELEMS = 1 << 20
 NOALLOC_STAGING_BYTES = 4 << 20
@@ -131,6 +132,9 @@ def lib() -> ctypes.CDLL:
         L.freqkv_check_attend_q8.argtypes = [QP, *four, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P]
         L.freqkv_attend_decode_mass.argtypes = [c_void_p, LP, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, I32P,
                                                 ctypes.c_float, ctypes.c_float, c_void_p]
+        L.freqkv_attend_mass.argtypes = [c_void_p, LP, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P, ctypes.c_float,
+                                         ctypes.c_float, c_void_p]
+        L.freqkv_check_attend_mass.argtypes = [LP, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, I32P]
         L.freqkv_evict.argtypes = [c_void_p, LP, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, I32P, I32P, c_int32, c_int32, c_void_p]
         L.freqkv_check_evict.argtypes = [LP, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, I32P, I32P, c_int32, c_int32]
         L.freqkv_last_error.argtypes = [c_void_p]
@@ -573,6 +577,21 @@ class Context:
                                              _stream_ptr(stream))
         self._check(st, "freqkv_attend_decode_mass")
         return out
+
+    def attend_mass(self, k: torch.Tensor, layer: int, q: torch.Tensor, mass: torch.Tensor, lens: list[int], rope_base: float = 10000.0,
+                    scale: float = 0.0, stream=None) -> torch.Tensor:
+        """Adds the softmax weights that a chunk's queries (dense bf16 [batch, q_heads, n_new, 128], before RoPE, at cache rows
+        [lens[b] - n_new, lens[b])) give to each row, summed over them and the query heads of each KV head, to ``mass`` (fp32
+        [batch, layers, kv_heads, capacity], in place).  Returns ``mass``."""
+        lay = layout_of(k)
+        if q.dim() != 4 or not q.is_contiguous() or q.dtype != k.dtype or q.shape[0] != lay.batch or \
+                q.shape[3] != lay.head_dim or q.shape[1] % lay.kv_heads != 0 or len(lens) != lay.batch:
+            raise FreqKVError(ERR_INVALID_ARG, "q must be dense [batch, q_heads, n_new, head_dim] in the cache dtype, lens one entry per sequence")
+        self._per_row(mass, k, torch.float32, "mass")
+        st = lib().freqkv_attend_mass(self._h, ctypes.byref(lay), k.data_ptr(), layer, q.data_ptr(), mass.data_ptr(), q.shape[1] // lay.kv_heads,
+                                      q.shape[2], (c_int32 * lay.batch)(*lens), rope_base, scale, _stream_ptr(stream))
+        self._check(st, "freqkv_attend_mass")
+        return mass
 
     def evict(self, k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, lens: list[int], kept_len: list[int], sink: int, recent: int,
               mass_out: torch.Tensor | None = None, kept_rows: torch.Tensor | None = None, stream=None) -> list[int]:

@@ -4,6 +4,8 @@
 
 #include "ctx.cuh"
 #include "evict.cuh"
+#include "mass.cuh"
+#include "prefill.cuh"
 
 using namespace freqkv;
 
@@ -57,6 +59,59 @@ freqkv_status freqkv_attend_decode_mass(freqkv_ctx* ctx, const freqkv_layout* la
     }
     ctx->kernels_launched += launched;
     return e == cudaSuccess ? FREQKV_OK : cuda_fail(ctx, e, "attend_decode_mass");
+}
+
+freqkv_status freqkv_check_attend_mass(const freqkv_layout* layout, const void* k, int32_t layer, const void* q, const float* mass,
+                                       int32_t q_heads_per_kv, int32_t n_new, const int32_t* lens)
+{
+    if (!lens) return FREQKV_ERR_INVALID_ARG;
+    freqkv_status st = check_layout(layout);
+    if (st != FREQKV_OK) return st;
+    if (!k || !q) return FREQKV_ERR_INVALID_ARG;
+    if (((uintptr_t)k | (uintptr_t)q) & 15) return FREQKV_ERR_UNSUPPORTED;
+    st = check_mass(mass);
+    if (st != FREQKV_OK) return st;
+    if (layer < 0 || layer >= layout->layers || q_heads_per_kv < 1 || n_new < 1) return FREQKV_ERR_INVALID_ARG;
+    if (!prefill_supported(layout->dtype, layout->head_dim, q_heads_per_kv) || (int64_t)layout->kv_heads * (q_heads_per_kv + 1) > 65535)
+        return FREQKV_ERR_UNSUPPORTED;
+    for (int32_t b = 0; b < layout->batch; ++b)
+        if (lens[b] < n_new || lens[b] > layout->capacity) return FREQKV_ERR_INVALID_ARG;
+    return FREQKV_OK;
+}
+
+freqkv_status freqkv_attend_mass(freqkv_ctx* ctx, const freqkv_layout* layout, const void* k, int32_t layer, const void* q, float* mass,
+                                 int32_t q_heads_per_kv, int32_t n_new, const int32_t* lens, float rope_base, float scale,
+                                 void* cuda_stream)
+{
+    if (!ctx) return FREQKV_ERR_INVALID_ARG;
+    const freqkv_status st = freqkv_check_attend_mass(layout, k, layer, q, mass, q_heads_per_kv, n_new, lens);
+    if (st != FREQKV_OK) return st;
+    if (!(scale == scale) || !(rope_base == rope_base)) return FREQKV_ERR_INVALID_ARG;  // NaN
+    const freqkv_layout& l = *layout;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return FREQKV_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    WorkOrder order(ctx, stream);
+    if (scale <= 0.f) scale = 1.0f / sqrtf((float)l.head_dim);
+    const float2* table = nullptr;
+    const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
+    if (ts != FREQKV_OK) return ts;
+    const freqkv_status gs = prefill_scratch(ctx, mass_key_bytes(l), mass_query_bytes(l, q_heads_per_kv, n_new));
+    if (gs != FREQKV_OK) return gs;
+    const char* why = nullptr;
+    int32_t launched = 0;
+    cudaError_t e;
+    {
+        TransformTimer timer(ctx, stream);
+        e = launch_attend_chunk_mass(l, k, layer, q, mass, q_heads_per_kv, n_new, lens, table, scale, ctx->prefill_keys, ctx->prefill_queries,
+                                     ctx->status_dev, ctx->gemm.wait_limit_ns, &why, &launched, stream);
+    }
+    ctx->kernels_launched += launched;
+    if (e == cudaSuccess) return FREQKV_OK;
+    if (!why) return cuda_fail(ctx, e, "attend_mass");
+    cudaGetLastError();
+    ctx->last_error = why;
+    return e == cudaErrorNotSupported ? FREQKV_ERR_UNSUPPORTED : FREQKV_ERR_CUDA;
 }
 
 freqkv_status freqkv_check_evict(const freqkv_layout* layout, const void* k, const void* v, const float* mass, const float* mass_out,

@@ -1,0 +1,412 @@
+// The attention weights that a chunk's queries give to the cache rows, added up per row over the chunk and the query heads
+// of each KV head: what eviction goes by, for prompts.  Positions and causality as in prefill.cu.
+//
+// A row's weight needs every query's maximum and sum first, so the scores are computed twice, both times on the tcgen05 tensor
+// cores and without going through memory:
+//   pass 1 (CUDA cores): keys of the layer and queries of the chunk are turned (RoPE, fp32) and written as two fp16 parts each,
+//     x = hi + lo with 22 bits: sums of weights are kept in fp32, and one fp16 part would leave 2^-11 a term in the scores.
+//     A score is  hi hi + hi lo + lo hi  (what is left out is 2^-22 of a term).
+//   pass 2, a CTA for each (sequence, query head, 128 queries): S = Q K^T over tiles of 128 keys; running maximum and sum of
+//     each query, one query a thread and half of the tile's columns;
+//   pass 3, a CTA for each (sequence, KV head, 128 keys): S^T = K Q^T over tiles of 128 queries of all heads of the group that see
+//     the keys; a thread has one key and adds up half of the columns' weights, so there are no sums across threads but the last.
+// Passes 2 and 3 are one kernel with its sides exchanged: 128 resident rows ("A"), 128 streamed rows a tile ("B", two
+// stages), the scores of two tiles in tensor memory, so that one tile's products run while the other's scores are read:
+//   warp 0 loads (TMA), warp 1 issues the products, warps 2-9 read scores, two warps a lane quarter, 64 columns each.
+// Bound by the tensor cores: 3 * 8 products of 128 x 128 x 16 a tile and pass.  Every wait is bounded as in prefill.cu.
+#include <algorithm>
+
+#include "mass.cuh"
+#include "tc_dev.cuh"
+
+namespace freqkv {
+namespace {
+
+constexpr int T = 128;                    // rows of A, rows of a B tile
+constexpr int SLAB = T * 128;             // bytes: 128 rows x 64 fp16 values, a 128-byte swizzle row each
+constexpr int OPERAND = 4 * SLAB;         // hi and lo, 128 channels
+constexpr int STAGES = 2;
+constexpr int OFF_A = 0, OFF_B = OPERAND, OFF_BAR = OFF_B + STAGES * OPERAND;
+constexpr int SMEM_BYTES = OFF_BAR + 256 + 2048 + 1024;  // barriers, the halves' merge, slack for the alignment
+constexpr int READERS = 8, THREADS = 64 + 32 * READERS;
+constexpr int TMEM_COLS = 2 * T;
+
+struct ChunkParams {
+    int32_t n_new, n_pad, kv_heads, g, batch0, batch_count, q_tiles, k_tiles;
+    float c;                // scale * log2(e)
+    float2* stats;          // [batch * heads_q][n_pad]: maximum * c, 1 / sum
+    float* mass;            // moved to the layer
+    int64_t mass_batch, mass_rows;
+    int32_t* status;
+    unsigned long long wait_limit_ns;
+    int32_t len[PREFILL_MAX_BATCH];
+};
+
+// ---- pass 1: rows of a half-warp each, as in prefill.cu, written as [slice][hi, lo][rows][128] ----
+struct SplitJob {
+    const __nv_bfloat16* k;
+    int64_t stride_batch, stride_head, stride_token;
+    const __nv_bfloat16* q;
+    __half* k_out;
+    __half* q_out;
+    const float2* table;
+    int32_t kv_heads, heads_q, n_new, capacity, k_rows, batch0, batch_count;
+    int32_t len[PREFILL_MAX_BATCH];
+};
+
+__device__ __forceinline__ uint32_t split2(float a, float b, uint32_t& lo)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - f.x, b - f.y);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__global__ void __launch_bounds__(256) mass_split_kernel(const __grid_constant__ SplitJob job)
+{
+    const int l16 = threadIdx.x % 16, c0 = 4 * l16;
+    const int32_t k_slices = job.batch_count * job.kv_heads;
+    const bool is_key = (int32_t)blockIdx.y < k_slices;
+    const int32_t slice = is_key ? (int32_t)blockIdx.y : (int32_t)blockIdx.y - k_slices;
+    const int32_t heads = is_key ? job.kv_heads : job.heads_q, b = slice / heads, hh = slice % heads;
+    const int32_t rows = is_key ? job.k_rows : job.n_new, len = job.len[b];
+    const int64_t bb = job.batch0 + b;
+    const __nv_bfloat16* src0 = is_key ? job.k + bb * job.stride_batch + (int64_t)hh * job.stride_head : job.q + (bb * job.heads_q + hh) * job.n_new * 128;
+    const int64_t src_stride = is_key ? job.stride_token : 128, all_rows = is_key ? job.capacity : job.n_new;
+    __half* dst0 = (is_key ? job.k_out : job.q_out) + (bb * heads + hh) * all_rows * 256;
+    const int32_t pos0 = is_key ? 0 : len - job.n_new;
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+        const int32_t row = (int32_t)blockIdx.x * 64 + (threadIdx.x / 16) * 4 + i4;
+        if (row >= rows) break;
+        float lo[4] = {0.f, 0.f, 0.f, 0.f}, hi[4] = {0.f, 0.f, 0.f, 0.f};
+        if (!(is_key && row >= len)) {  // key rows from the length on are written as zeros
+            const __nv_bfloat16* src = src0 + (int64_t)row * src_stride;
+            const uint2 a = __ldg(reinterpret_cast<const uint2*>(src + c0)), c = __ldg(reinterpret_cast<const uint2*>(src + 64 + c0));
+            lo[0] = __uint_as_float(a.x << 16); lo[1] = __uint_as_float(a.x & 0xffff0000u);
+            lo[2] = __uint_as_float(a.y << 16); lo[3] = __uint_as_float(a.y & 0xffff0000u);
+            hi[0] = __uint_as_float(c.x << 16); hi[1] = __uint_as_float(c.x & 0xffff0000u);
+            hi[2] = __uint_as_float(c.y << 16); hi[3] = __uint_as_float(c.y & 0xffff0000u);
+            if (job.table) {
+                const float4* t = reinterpret_cast<const float4*>(job.table + (int64_t)(pos0 + row) * 64 + c0);
+                const float4 t0 = __ldg(t), t1 = __ldg(t + 1);
+                rotate(lo[0], hi[0], make_float2(t0.x, t0.y));
+                rotate(lo[1], hi[1], make_float2(t0.z, t0.w));
+                rotate(lo[2], hi[2], make_float2(t1.x, t1.y));
+                rotate(lo[3], hi[3], make_float2(t1.z, t1.w));
+            }
+        }
+        uint2 h, r;
+        __half* dst = dst0 + (int64_t)row * 128;
+        h.x = split2(lo[0], lo[1], r.x);
+        h.y = split2(lo[2], lo[3], r.y);
+        *reinterpret_cast<uint2*>(dst + c0) = h;
+        *reinterpret_cast<uint2*>(dst + all_rows * 128 + c0) = r;
+        h.x = split2(hi[0], hi[1], r.x);
+        h.y = split2(hi[2], hi[3], r.y);
+        *reinterpret_cast<uint2*>(dst + 64 + c0) = h;
+        *reinterpret_cast<uint2*>(dst + all_rows * 128 + 64 + c0) = r;
+    }
+}
+
+// ---- passes 2 and 3 ----
+constexpr uint32_t IDESC = (1u << 4) | (0u << 7) | (0u << 10) | (0u << 15) | (0u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);  // fp16 in, fp32 out
+
+template <bool SUMS>
+__global__ void __launch_bounds__(THREADS, 1)
+mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ ChunkParams prm)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* aligned = smem_raw + (base - raw);
+    const uint32_t bar0 = base + OFF_BAR, a_full = bar0;
+    auto b_full = [&](int s) { return bar0 + 8u * (1 + s); };
+    auto b_empty = [&](int s) { return bar0 + 8u * (1 + STAGES + s); };
+    auto d_full = [&](int s) { return bar0 + 8u * (1 + 2 * STAGES + s); };
+    auto d_free = [&](int s) { return bar0 + 8u * (3 + 2 * STAGES + s); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + OFF_BAR + 8 * (5 + 2 * STAGES));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    float2* sm_half = reinterpret_cast<float2*>(aligned + OFF_BAR + 256);  // [128]: what the second half's threads have found
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int32_t heads_q = prm.kv_heads * prm.g;
+    // which rows are resident, and over which tiles the others run
+    int32_t b, h, row0, first_tile, n_tiles, q_head = 0;
+    if constexpr (SUMS) {
+        const int32_t units = prm.kv_heads * prm.batch_count, unit = (int32_t)blockIdx.x % units;
+        b = unit / prm.kv_heads;
+        h = unit % prm.kv_heads;
+        row0 = (int32_t)blockIdx.x / units * T;
+    } else {  // the query tiles with the most keys first
+        const int32_t units = heads_q * prm.batch_count, unit = (int32_t)blockIdx.x % units;
+        b = unit / heads_q;
+        q_head = unit % heads_q;
+        h = q_head / prm.g;
+        row0 = (prm.q_tiles - 1 - (int32_t)blockIdx.x / units) * T;
+    }
+    const int32_t len = prm.len[b], pos0 = len - prm.n_new;
+    if constexpr (SUMS) {
+        if (row0 >= len) return;  // a shorter sequence
+        first_tile = row0 > pos0 ? (row0 - pos0) / T : 0;
+        n_tiles = (prm.q_tiles - first_tile) * prm.g;
+    } else {
+        first_tile = 0;
+        n_tiles = (pos0 + min(row0 + T, prm.n_new) - 1) / T + 1;
+    }
+    const int32_t per_head = prm.q_tiles - first_tile;  // SUMS: tiles of a head
+    const int32_t k_slice = (prm.batch0 + b) * prm.kv_heads + h, q_slice0 = (prm.batch0 + b) * heads_q;
+
+    if (threadIdx.x == 0) {
+        mbar_init(a_full, 1);
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(b_full(s), 1);
+            mbar_init(b_empty(s), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(d_full(s), 1);
+            mbar_init(d_free(s), READERS);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem_base = *tmem_slot;
+    // launched with programmatic stream serialization: what is above may run while the pass before drains
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if (warp == 0) {
+        if (lane == 0) {
+            auto load_operand = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t row, int32_t slice) {
+                mbar_expect_tx(bar, OPERAND);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tma_load_3d(dst + i * SLAB, map, bar, (i & 1) * 64, row, 2 * slice + i / 2);  // hi, then lo; 64 channels each
+            };
+            if (SUMS)
+                load_operand(base + OFF_A, &map_k, a_full, row0, k_slice);
+            else
+                load_operand(base + OFF_A, &map_q, a_full, row0, q_slice0 + q_head);
+            for (int32_t t = 0; t < n_tiles; ++t) {
+                const int s = t % STAGES;
+                if (t >= STAGES && !mbar_wait(b_empty(s), ((uint32_t)(t / STAGES) - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
+                if (SUMS)
+                    load_operand(base + OFF_B + s * OPERAND, &map_q, b_full(s), (first_tile + t % per_head) * T, q_slice0 + h * prm.g + t / per_head);
+                else
+                    load_operand(base + OFF_B + s * OPERAND, &map_k, b_full(s), t * T, k_slice);
+            }
+            if (*abort_flag) {  // let the copies in flight land before this CTA's shared memory goes away
+                const unsigned long long t0 = global_timer_ns();
+                while (global_timer_ns() - t0 < LANDING_NS) __nanosleep(1000);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && mbar_wait(a_full, 0, abort_flag, prm.status, prm.wait_limit_ns)) {
+            for (int32_t t = 0; t < n_tiles; ++t) {
+                const int s = t % STAGES, d = t & 1;
+                if (!mbar_wait(b_full(s), (uint32_t)(t / STAGES) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
+                if (t >= 2 && !mbar_wait(d_free(d), ((uint32_t)(t / 2) - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t aa = base + OFF_A, ba = base + OFF_B + s * OPERAND;
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {  // lo hi, hi lo, hi hi: the small ones first
+                    const uint32_t a_at = aa + (part == 0 ? 2 * SLAB : 0), b_at = ba + (part == 1 ? 2 * SLAB : 0);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        umma(tmem_base + d * T, smem_desc(a_at + (kk / 4) * SLAB + (kk % 4) * 32, 16, 1024),
+                             smem_desc(b_at + (kk / 4) * SLAB + (kk % 4) * 32, 16, 1024), IDESC, (part | kk) != 0);
+                }
+                umma_commit(d_full(d));
+                umma_commit(b_empty(s));
+            }
+        }
+    } else {
+        const int quarter = warp % 4, half = (warp - 2) / 4, row = quarter * 32 + lane;  // tensor-memory lane = row of A
+        const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 64;
+        const float c = prm.c;
+        float m = -1.0e30f;                       // pass 2: running maximum (of scores) and sum
+        float total[4] = {0.f, 0.f, 0.f, 0.f};    // pass 2: the sum in [0]; pass 3: four chains of the row's weight
+        bool alive = true;
+        for (int32_t t = 0; t < n_tiles; ++t) {
+            const int d = t & 1;
+            // pass 3: the maxima and sums of the tile's queries
+            const int32_t q0 = SUMS ? (first_tile + t % per_head) * T + half * 64 : 0;
+            const float2* stats = SUMS ? prm.stats + (int64_t)(q_slice0 + h * prm.g + t / per_head) * prm.n_pad + q0 : nullptr;
+            if (!mbar_wait(d_full(d), (uint32_t)(t / 2) & 1, abort_flag, prm.status, prm.wait_limit_ns)) {
+                alive = false;
+                break;
+            }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            uint32_t sc[64];
+            tmem_ld32<0>(from + d * T, sc);
+            tmem_ld32<32>(from + d * T + 32, sc);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(d_free(d));
+            if constexpr (SUMS) {
+                const int32_t key = row0 + row;
+                if (pos0 + q0 < row0 + quarter * 32 + 31) {  // some queries come before some keys of this warp: those do not see them
+#pragma unroll
+                    for (int j = 0; j < 64; ++j)
+                        if (key > pos0 + q0 + j) sc[j] = __float_as_uint(-INFINITY);
+                }
+#pragma unroll
+                for (int j = 0; j < 64; j += 2) {
+                    const float4 st = load(reinterpret_cast<const float4*>(stats + j));
+                    total[j / 2 & 3] = fmaf(ex2(fmaf(__uint_as_float(sc[j]), c, -st.x)), st.y, total[j / 2 & 3]);
+                    total[j / 2 & 3] = fmaf(ex2(fmaf(__uint_as_float(sc[j + 1]), c, -st.z)), st.w, total[j / 2 & 3]);
+                }
+            } else {
+                const int32_t j0 = t * T + half * 64, pos = pos0 + row0 + row;
+                if (j0 + 63 > pos0 + row0 + quarter * 32) {
+#pragma unroll
+                    for (int j = 0; j < 64; ++j)
+                        if (j0 + j > pos) sc[j] = __float_as_uint(-INFINITY);
+                }
+                float m4[4] = {m, m, m, m};
+#pragma unroll
+                for (int j = 0; j < 64; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], __uint_as_float(sc[j]), __uint_as_float(sc[j + 1]));
+                const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                const float mc = mx * c;
+                float s4[4] = {total[0] * ex2(fmaf(m, c, -mc)), 0.f, 0.f, 0.f};
+                m = mx;
+#pragma unroll
+                for (int j = 0; j < 64; ++j) s4[j & 3] += ex2(fmaf(__uint_as_float(sc[j]), c, -mc));
+                total[0] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            }
+        }
+        if (half == 1) sm_half[row] = SUMS ? make_float2((total[0] + total[1]) + (total[2] + total[3]), 0.f) : make_float2(m, total[0]);
+        asm volatile("bar.sync 1, %0;" ::"r"(32 * READERS) : "memory");
+        if (half == 0 && alive) {
+            const float2 o = sm_half[row];
+            if constexpr (SUMS) {
+                if (row0 + row < len) {
+                    float* at = prm.mass + (int64_t)(prm.batch0 + b) * prm.mass_batch + h * prm.mass_rows + row0 + row;
+                    *at += (total[0] + total[1]) + (total[2] + total[3]) + o.x;
+                }
+            } else {
+                const float mc = fmaxf(m, o.x) * c, l = total[0] * ex2(fmaf(m, c, -mc)) + o.y * ex2(fmaf(o.x, c, -mc));
+                // queries past the chunk's last one: no weight
+                prm.stats[(int64_t)(q_slice0 + q_head) * prm.n_pad + row0 + row] = row0 + row < prm.n_new ? make_float2(mc, 1.f / l) : make_float2(0.f, 0.f);
+            }
+        }
+    }
+
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS));
+    }
+}
+
+int32_t padded(int32_t n_new) { return (n_new + T - 1) / T * T; }
+
+}  // namespace
+
+size_t mass_key_bytes(const freqkv_layout& l) { return (size_t)l.batch * l.kv_heads * l.capacity * 512; }
+
+size_t mass_query_bytes(const freqkv_layout& l, int32_t q_heads_per_kv, int32_t n_new)
+{
+    return (size_t)l.batch * l.kv_heads * q_heads_per_kv * ((size_t)n_new * 512 + (size_t)padded(n_new) * sizeof(float2));
+}
+
+cudaError_t launch_attend_chunk_mass(const freqkv_layout& l, const void* k, int32_t layer, const void* q, float* mass, int32_t g, int32_t n_new,
+                                     const int32_t* lens_host, const float2* table, float scale, void* key_scratch, void* query_scratch,
+                                     int32_t* status, unsigned long long wait_limit_ns, const char** error, int32_t* kernels_launched,
+                                     cudaStream_t stream)
+{
+    *error = nullptr;
+    if (!encode_fn()) {
+        *error = "cuTensorMapEncodeTiled is not available from this driver";
+        return cudaErrorNotSupported;
+    }
+    static PerDeviceOnce attrs;
+    const cudaError_t attr_error = attrs.run([] {
+        cudaError_t e = cudaFuncSetAttribute(mass_tiles_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(mass_tiles_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+        return e;
+    });
+    if (attr_error != cudaSuccess) return attr_error;
+    const int32_t heads_q = l.kv_heads * g;
+    __half* keys = static_cast<__half*>(key_scratch);
+    __half* queries = static_cast<__half*>(query_scratch);
+    CUtensorMap map_q, map_k;
+    if (!encode_rows_map(&map_q, queries, n_new, (int64_t)l.batch * heads_q * 2, T) ||
+        !encode_rows_map(&map_k, keys, l.capacity, (int64_t)l.batch * l.kv_heads * 2, T)) {
+        *error = "cuTensorMapEncodeTiled rejected a tensor of the attention weights";
+        return cudaErrorInvalidValue;
+    }
+    const int32_t per_launch = std::max(1, std::min(PREFILL_MAX_BATCH, 65535 / (l.kv_heads + heads_q)));
+    for (int32_t b0 = 0; b0 < l.batch; b0 += per_launch) {
+        const int32_t nb = std::min(per_launch, l.batch - b0);
+        SplitJob job;
+        job.k = static_cast<const __nv_bfloat16*>(k) + (int64_t)layer * l.stride_layer;
+        job.stride_batch = l.stride_batch;
+        job.stride_head = l.stride_head;
+        job.stride_token = l.stride_token;
+        job.q = static_cast<const __nv_bfloat16*>(q);
+        job.k_out = keys;
+        job.q_out = queries;
+        job.table = table;
+        job.kv_heads = l.kv_heads;
+        job.heads_q = heads_q;
+        job.n_new = n_new;
+        job.capacity = l.capacity;
+        job.batch0 = b0;
+        job.batch_count = nb;
+        ChunkParams prm;
+        int32_t max_len = 0;
+        for (int32_t i = 0; i < nb; ++i) {
+            job.len[i] = prm.len[i] = lens_host[b0 + i];
+            max_len = std::max(max_len, lens_host[b0 + i]);
+        }
+        job.k_rows = std::min(l.capacity, (max_len + T - 1) / T * T);
+        const dim3 split_grid((unsigned)((std::max(job.k_rows, n_new) + 63) / 64), (unsigned)(nb * (l.kv_heads + heads_q)));
+        mass_split_kernel<<<split_grid, 256, 0, stream>>>(job);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        prm.n_new = n_new;
+        prm.n_pad = padded(n_new);
+        prm.kv_heads = l.kv_heads;
+        prm.g = g;
+        prm.batch0 = b0;
+        prm.batch_count = nb;
+        prm.q_tiles = prm.n_pad / T;
+        prm.k_tiles = (max_len + T - 1) / T;
+        prm.c = scale * 1.4426950408889634f;
+        prm.stats = reinterpret_cast<float2*>(queries + (int64_t)l.batch * heads_q * n_new * 256);
+        prm.mass = mass + (int64_t)layer * l.kv_heads * l.capacity;
+        prm.mass_batch = (int64_t)l.layers * l.kv_heads * l.capacity;
+        prm.mass_rows = l.capacity;
+        prm.status = status;
+        prm.wait_limit_ns = wait_limit_ns;
+        cudaLaunchConfig_t cfg = {};
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = SMEM_BYTES;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;  // let each launch overlap the tail of the one before
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        cfg.gridDim = dim3((unsigned)((int64_t)prm.q_tiles * heads_q * nb));
+        e = cudaLaunchKernelEx(&cfg, mass_tiles_kernel<false>, map_q, map_k, prm);
+        if (e != cudaSuccess) return e;
+        cfg.gridDim = dim3((unsigned)((int64_t)prm.k_tiles * l.kv_heads * nb));
+        e = cudaLaunchKernelEx(&cfg, mass_tiles_kernel<true>, map_q, map_k, prm);
+        if (e != cudaSuccess) return e;
+        *kernels_launched += 3;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace freqkv

@@ -158,6 +158,97 @@ def test_decode_mass_refusals(ctx):
     assert not bool(mass.any())
 
 
+# ---- a chunk's weights ----
+
+def check_chunk(ctx, k, layer, q, lens, base=10000.0, scale=0.0, heads=None):
+    B, L, H, cap, _ = k.shape
+    G, n = q.shape[1] // H, q.shape[2]
+    start = masses((B, L, H, cap), 3) * 0.01
+    mass = start.clone()
+    ctx.attend_mass(k, layer, q, mass, lens, rope_base=base, scale=scale)
+    assert ctx.last_device_status() == fk.OK
+    for b, h in heads or np.ndindex(B, H):
+        want = oe.weights(parity.to_f64(q[b, h * G:(h + 1) * G]), parity.to_f64(k[b, layer, h]), lens[b], base, None if scale <= 0 else scale)
+        got = parity.to_f64(mass[b, layer, h, :lens[b]])
+        assert parity.rel_l2(got, parity.to_f64(start[b, layer, h, :lens[b]]) + want) <= WEIGHTS
+        assert torch.equal(mass[b, layer, h, lens[b]:], start[b, layer, h, lens[b]:])
+    mass[:, layer] = start[:, layer]
+    assert torch.equal(mass, start)
+
+
+@pytest.mark.parametrize("G,n,lens", [(1, 1, [1, 70]), (2, 2, [2, 3]), (3, 64, [64, 200]), (4, 129, [129, 300]), (1, 200, [230, 299]),
+                                      (9, 5, [65, 128]), (2, 127, [127, 255]), (1, 128, [128, 256]), (8, 17, [257, 300])])
+def test_chunk_mass_small(ctx, G, n, lens):
+    k, _ = caches(2, 2, 2, 300, torch.bfloat16, n)
+    check_chunk(ctx, k, 1, queries((2, 2 * G, n, 128), torch.bfloat16, n), lens)
+
+
+@pytest.mark.parametrize("base,scale", [(0.0, 0.0), (500000.0, 0.05)])
+def test_chunk_mass_rope_off_other_base_and_scale(ctx, base, scale):
+    k, _ = caches(1, 1, 2, 500, torch.bfloat16, 21)
+    check_chunk(ctx, k, 0, queries((1, 4, 130, 128), torch.bfloat16, 3), [497], base, scale)
+
+
+def test_chunk_mass_padded_rows_many_sequences_and_what_lies_behind(ctx):
+    w = synth.Workload("evict", 1, 1, 2, 128, 700, torch.bfloat16, 4, 0.9, 2, synth.BASE_SEED + 13)
+    (_, k), _ = parity.guarded_cache(w, torch.device("cuda"), fill_len=700, row_pad=8)
+    q = queries((1, 2, 300, 128), torch.bfloat16, 6)
+    check_chunk(ctx, k, 0, q, [600])
+    a, b = torch.zeros(1, 1, 2, 700, device="cuda"), torch.zeros(1, 1, 2, 700, device="cuda")
+    ctx.attend_mass(k, 0, q, a, [600])
+    k[..., 600:, :] = float("nan")
+    ctx.attend_mass(k, 0, q, b, [600])
+    assert torch.equal(a, b)
+    B = 130
+    k, _ = caches(B, 1, 1, 40, torch.bfloat16, 15)
+    check_chunk(ctx, k, 0, queries((B, 2, 3, 128), torch.bfloat16, 6), [3 + (11 * i) % 38 for i in range(B)])
+
+
+def test_chunk_mass_of_one_token_is_that_of_decoding(ctx):
+    k, v = caches(2, 1, 2, 1777, torch.bfloat16, 23)
+    q = queries((2, 8, 128), torch.bfloat16, 4)
+    a, b = torch.zeros(2, 1, 2, 1777, device="cuda"), torch.zeros(2, 1, 2, 1777, device="cuda")
+    ctx.attend_decode_mass(k, v, 0, q, a, [1777, 5])
+    ctx.attend_mass(k, 0, q.unsqueeze(2).contiguous(), b, [1777, 5])
+    assert float((a - b).norm() / a.norm()) <= 2 * WEIGHTS
+
+
+def test_chunk_mass_large_against_64_bits_on_the_gpu(ctx):
+    """Many tiles a CTA: the weights of 1500 queries over 6000 rows, in 64-bit torch."""
+    n, T = 1500, 6000
+    k, _ = caches(1, 1, 2, T, torch.bfloat16, 24)
+    q = queries((1, 6, n, 128), torch.bfloat16, 4)
+    mass = torch.zeros(1, 1, 2, T, device="cuda")
+    ctx.attend_mass(k, 0, q, mass, [T])
+    turn = torch.polar(torch.ones((), dtype=torch.float64, device="cuda"),
+                       torch.arange(T, device="cuda").double()[:, None] * 10000.0 ** (-torch.arange(64, device="cuda").double() / 64))
+    z = lambda x, at: torch.complex(x[..., :64].double(), x[..., 64:].double()) * at
+    hidden = torch.full((n, T), -torch.inf, dtype=torch.float64, device="cuda").triu(T - n + 1)
+    for h in range(2):
+        s = (z(q[0, 3 * h:3 * h + 3], turn[T - n:]) @ z(k[0, 0, h], turn).conj().T).real / 128 ** 0.5 + hidden
+        want = torch.softmax(s, -1).sum((0, 1))
+        assert float((mass[0, 0, h].double() - want).norm() / want.norm()) <= 2e-5
+        assert abs(float(mass[0, 0, h].double().sum()) / (3 * n) - 1) <= 2e-6
+
+
+def test_chunk_mass_captured_and_refused(ctx):
+    k, _ = caches(1, 2, 2, 300, torch.bfloat16, 25)
+    q, mass = queries((1, 4, 70, 128), torch.bfloat16, 4), torch.zeros(1, 2, 2, 300, device="cuda")
+    ctx.attend_mass(k, 1, q, mass, [222])
+    once = mass.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.attend_mass(k, 1, q, mass, [222])
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(mass, 2 * once)
+    for kw in ({"lens": [69]}, {"lens": [301]}, {"layer": 2}, {"scale": float("nan")}, {"mass": mass[..., :32]}, {"q": q.float()}, {"k": k.float()}):
+        a = dict(k=k, layer=0, q=q, mass=mass, lens=[222]) | kw
+        with pytest.raises(fk.FreqKVError):
+            ctx.attend_mass(**a)
+    assert torch.equal(mass, 2 * once)
+
+
 # ---- eviction ----
 
 def check_evict(ctx, k, v, mass, lens, kept, sink, recent, in_place=True, with_rows=True):
@@ -272,3 +363,41 @@ def test_evict_refusals(ctx):
         with pytest.raises(fk.FreqKVError):
             ctx.evict(**a)
     assert torch.equal(k, k0) and torch.equal(mass, m0)
+
+
+def test_a_stream_with_eviction(ctx):
+    """As they are used: a prompt in chunks, then tokens, weights added up all the way, the full cache evicted twice: the rows that
+    stay are the oracle's choice by the masses, and every query has given away a weight of one."""
+    B, L, H, cap, G, sink, recent = 2, 2, 2, 256, 4, 4, 32
+    k, v = (torch.zeros(B, L, H, cap, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    mass, lens, seed = torch.zeros(B, L, H, cap, device="cuda"), [0] * B, 70
+    for n in (128, 128, None, 100, 1, 1, 24, None, 1, 1):
+        seed += 1
+        if n is None:
+            with pytest.raises(fk.FreqKVError) as e:
+                ctx.append(k, v, new[0][:, :, :, :1].contiguous(), new[1][:, :, :, :1].contiguous(), lens)
+            assert e.value.status == fk.ERR_CAPACITY
+            assert abs(float(mass.double().sum()) - seen) <= 1e-4 * seen
+            k0, v0, m0, had = k.clone(), v.clone(), mass.clone(), lens
+            kept = [(x - sink) // 2 for x in lens]
+            lens = ctx.evict(k, v, mass, lens, kept, sink, recent)
+            m_host = m0.double().cpu().numpy()
+            for b, l, h in np.ndindex(B, L, H):
+                idx = torch.tensor(oe.keep(m_host[b, l, h], had[b], kept[b], sink, recent), device="cuda")
+                assert torch.equal(k[b, l, h, :lens[b]], k0[b, l, h][idx]) and torch.equal(v[b, l, h, :lens[b]], v0[b, l, h][idx])
+                assert torch.equal(mass[b, l, h, :lens[b]], m0[b, l, h][idx]) and not bool(mass[b, l, h, lens[b]:].any())
+            continue
+        seen = float(mass.double().sum()) + B * L * H * G * n      # every query gives away one
+        new = [queries((B, L, H, n, 128), torch.bfloat16, seed + 100 * i) for i in range(2)]
+        lens = ctx.append(k, v, *new, lens)
+        for layer in range(L):
+            q = queries((B, H * G, n, 128), torch.bfloat16, seed + layer)
+            if n == 1:
+                one = q[:, :, 0].contiguous()
+                a, b = ctx.attend_decode_mass(k, v, layer, one, mass, lens), ctx.attend_decode(k, v, layer, one, lens)
+                assert float((a.float() - b.float()).norm() / b.float().norm()) <= 2 * OUT[torch.bfloat16]
+            else:
+                ctx.attend_prefill(k, v, layer, q, lens)
+                ctx.attend_mass(k, layer, q, mass, lens)
+        assert abs(float(mass.double().sum()) - seen) <= 1e-4 * seen
+    assert ctx.last_device_status() == fk.OK

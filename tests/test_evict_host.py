@@ -54,6 +54,21 @@ def test_check_evict_pointers():
         assert check(*ok, layout=lay(hd=hd, dtype=fk.F32)) == fk.OK
 
 
+def test_check_attend_mass():
+    def mass(lens=(10, 64), layer=0, k=K, q=V, m=M, G=2, n=5, layout=None):
+        return fk.lib().freqkv_check_attend_mass(ctypes.byref(layout or lay()), k, layer, q, m, G, n, (ctypes.c_int32 * 2)(*lens))
+
+    assert mass() == fk.OK
+    assert mass(G=64) == fk.OK and mass(G=65) == fk.ERR_UNSUPPORTED and mass(G=0) == fk.ERR_INVALID_ARG
+    assert mass(n=0) == fk.ERR_INVALID_ARG and mass(n=11) == fk.ERR_INVALID_ARG and mass(n=10) == fk.OK
+    assert mass(lens=(10, 257)) == fk.ERR_INVALID_ARG
+    assert mass(layer=2) == fk.ERR_INVALID_ARG and mass(layer=-1) == fk.ERR_INVALID_ARG
+    for name in ("k", "q", "m"):
+        assert mass(**{name: 0}) == fk.ERR_INVALID_ARG
+    assert mass(k=K + 8) == fk.ERR_UNSUPPORTED and mass(m=M + 2) == fk.ERR_UNSUPPORTED
+    assert mass(layout=lay(dtype=fk.F32)) == fk.ERR_UNSUPPORTED and mass(layout=lay(hd=64)) == fk.ERR_UNSUPPORTED
+
+
 def test_null_context():
     lib, layout, one = fk.lib(), lay(B=1), (ctypes.c_int32 * 1)(100)
     assert lib.freqkv_evict(None, ctypes.byref(layout), K, V, M, M, None, one, one, 4, 8, None) == fk.ERR_INVALID_ARG
