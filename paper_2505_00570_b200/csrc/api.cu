@@ -126,7 +126,7 @@ freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base,
             ctx->rope_table = nullptr;
         }
         const int32_t rows = std::max(capacity, 2);
-        FREQKV_CUDA(ctx, cudaMalloc(&ctx->rope_table, (size_t)rows * 64 * sizeof(float2)));
+        FREQKV_CUDA(ctx, cudaMalloc(&ctx->rope_table, rope_table_bytes(rows)));
         const cudaError_t e = launch_rope_table(ctx->rope_table, rows, (double)rope_base, stream);
         if (e != cudaSuccess) return cuda_fail(ctx, e, "rope_table");
         ctx->rope_rows = rows;

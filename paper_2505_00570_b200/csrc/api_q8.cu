@@ -226,7 +226,7 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
     WorkOrder order(ctx, stream);
     if (scale <= 0.f) scale = 1.0f / sqrtf((float)l.head_dim);
     const float2* table = nullptr;
-    const freqkv_status ts = rope_table_for(ctx, std::max(l.capacity, 16), rope_base, stream, &table);
+    const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
     AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads * q8_head_groups(q_heads_per_kv), attend_q8_resident(ctx->sm_count), lens);
     plan.captured = is_capturing(stream);
@@ -237,7 +237,8 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
     cudaError_t e;
     {
         TransformTimer timer(ctx, stream);
-        e = launch_attend_q8(q8_view(l, k, v, k_scale, v_scale), l.batch, layer, q, out, q_heads_per_kv, lens, table, scale, plan, work.partial,
+        e = launch_attend_q8(q8_view(l, k, v, k_scale, v_scale), l.batch, layer, q, out, q_heads_per_kv, lens, table,
+                             table ? reinterpret_cast<const uint4*>(table + (int64_t)ctx->rope_rows * 64) : nullptr, scale, plan, work.partial,
                              work.tickets, &launched, stream);
     }
     ctx->kernels_launched += launched;
@@ -259,7 +260,7 @@ freqkv_status freqkv_attend_prefill_q8(freqkv_ctx* ctx, const freqkv_q8_layout* 
     WorkOrder order(ctx, stream);
     if (scale <= 0.f) scale = 1.0f / sqrtf((float)l.head_dim);
     const float2* table = nullptr;
-    const freqkv_status ts = rope_table_for(ctx, std::max(l.capacity, 16), rope_base, stream, &table);
+    const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
     const Q8View view = q8_view(l, k, v, k_scale, v_scale);
     const freqkv_status gs = prefill_scratch(ctx, prefill_q8_scratch_bytes(view, l.batch, l.capacity),

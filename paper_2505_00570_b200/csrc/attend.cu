@@ -413,12 +413,6 @@ static_assert(MMA_WARPS * 8 * (128 + 2) * 4 <= MMA_SMEM_BYTES, "the merge of the
 
 __device__ __forceinline__ uint32_t tile_off(int row, int chunk) { return (uint32_t)(row * 256 + ((chunk ^ (row & 7)) << 4)); }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid)
-{
-    const int bytes = valid ? 16 : 0;  // 0 source bytes: the 16 destination bytes are zero-filled
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-
 template <int G, bool TICKETS>
 __global__ void __launch_bounds__(MMA_THREADS, MMA_CTAS_PER_SM) attend_mma_kernel(const AttendParams p)
 {
@@ -749,14 +743,23 @@ __global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_
 }
 
 // cos / sin of pos * base^(-2c/128) in fp64, rounded once.
+// Behind it, rows 0 .. ROPE_HALF_ROWS - 1 once more as fp16: 64 cosines, then 64 sines.
 __global__ void rope_table_kernel(float2* table, int32_t rows, double base)
 {
-    const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= (int64_t)rows * 64) return;
+    int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const bool halves = i >= (int64_t)rows * 64;
+    __half* half_rows = reinterpret_cast<__half*>(table + (int64_t)rows * 64);
+    if (halves) i -= (int64_t)rows * 64;
+    if (halves && i >= ROPE_HALF_ROWS * 64) return;
     const int32_t pos = (int32_t)(i / 64), c = (int32_t)(i % 64);
     const double angle = (double)pos * pow(base, -2.0 * c / 128.0);
     double sn, cs;
     sincos(angle, &sn, &cs);
+    if (halves) {
+        half_rows[pos * 128 + c] = __double2half(cs);
+        half_rows[pos * 128 + 64 + c] = __double2half(sn);
+        return;
+    }
     table[i] = make_float2((float)cs, (float)sn);
 }
 
@@ -902,7 +905,7 @@ size_t attend_partial_bytes(int32_t splits, int32_t batch, int32_t q_heads)
 
 cudaError_t launch_rope_table(float2* table, int32_t rows, double base, cudaStream_t stream)
 {
-    const int64_t n = (int64_t)rows * 64;
+    const int64_t n = (int64_t)(rows + ROPE_HALF_ROWS) * 64;
     rope_table_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(table, rows, base);
     return cudaGetLastError();
 }

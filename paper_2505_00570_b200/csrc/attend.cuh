@@ -24,7 +24,10 @@ int32_t attend_most_splits(int32_t longest);
 // after every launch; the splits' partials.
 size_t attend_ticket_bytes(int sm_count);
 size_t attend_partial_bytes(int32_t splits, int32_t batch, int32_t q_heads);
-// table[pos][c] = (cos, sin)(pos * base^(-2c/128)), pos < rows, c < 64.
+// table[pos][c] = (cos, sin)(pos * base^(-2c/128)), pos < rows, c < 64; behind it rows 0 .. ROPE_HALF_ROWS - 1 as fp16, 64 cosines and 64
+// sines each.
+constexpr int ROPE_HALF_ROWS = 64;
+inline size_t rope_table_bytes(int32_t rows) { return (size_t)rows * 64 * sizeof(float2) + ROPE_HALF_ROWS * 256; }
 cudaError_t launch_rope_table(float2* table, int32_t rows, double base, cudaStream_t stream);
 // q, out: [batch, kv_heads * g, 128] in the cache dtype; table may be null (no RoPE).
 cudaError_t launch_attend(const freqkv_layout& l, const void* k, const void* v, int32_t layer, const void* q, void* out,

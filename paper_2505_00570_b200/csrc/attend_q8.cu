@@ -6,13 +6,15 @@
 //  - Codes go from memory into registers in the layout that the matrix instruction (mma.sync m16n8k16, fp32 accumulation) wants,
 //    without shared memory.  The order of the contraction index is free, so a lane's share of a key row is 16 consecutive
 //    channels and the 16 that RoPE pairs with them (two 16-byte loads), and its share of four value rows is 16 channels each.
-//    The next tile's loads are in flight while a tile is computed.
+//    A tile's keys make room for the next one's as soon as its scores are there, its values after the second product.
 //  - Codes become fp16 exactly (e4m3: one conversion of two; int8: a byte permute and a subtraction of two).  For V, whose rows are
 //    the contraction index, the bytes of two rows are interleaved before the conversion.
-//  - RoPE: the score of key row j0 + r (j0 the tile's first row) and the query at len - 1 is  k . R(len - 1 - j0 - r) q, and is
-//    computed as  (R(r) k) . (R(len - 1 - j0) q): the key rows of every tile are turned by the same 16 angles, whose cosines
-//    and sines lie in shared memory as fp16, two channels an instruction; the queries (8 heads, one column of the instruction
-//    each) are turned once a tile, in fp32, straight from the table of the context.
+//  - RoPE: the score of key row j0 + r and the query at len - 1 is  k . R(len - 1 - j0 - r) q, and is computed as
+//    (R(r) k) . (R(len - 1 - j0) q)  with j0 the first row of four tiles: the key rows of every 64 are turned by the same angles,
+//    whose cosines and sines lie in shared memory as fp16, two channels an instruction; the queries (8 heads, one column of
+//    the matrix instruction each) are turned once in 64 rows, in fp32, by the context's table, whose row comes ahead of time.
+//    (Turned once in 16 rows, with loads where they are used, 8 layers of 8 x 8 heads took 408 us: 340 wavefronts of shared
+//    memory and L1 a tile, and a wait for L2 in each.)
 //  - The block's scale of K multiplies the scores, that of V the softmax weights, which are rounded to fp16 as multiples of
 //    the largest V scale so far (`vref`), so that any scales' range will do.
 // Rounding: turned keys and queries to fp16 (cosine, product, sum: 4 roundings of 2^-11 at most each), weights to fp16; all
@@ -28,12 +30,17 @@
 namespace freqkv {
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, CTAS_PER_SM = 3;
+constexpr int WARPS = 4, THREADS = 32 * WARPS, CTAS_PER_SM = 4;
 static_assert(CTAS_PER_SM <= ATTEND_MOST_CTAS_PER_SM, "tickets");
 constexpr int TILE = 16;
+constexpr int TURN_TILES = 4;                 // tiles whose queries are turned alike
+constexpr int TURN_ROWS = TURN_TILES * TILE;
 constexpr int CS_ROW = 17;   // uint4 per row of the cosines and sines: 8 + 8, and one to spread the rows over the banks
 constexpr int Q_ROW = 36;    // float4 per head: 32, and 4 likewise
 constexpr int O_ROW = 132;   // floats per head of the warps' merge
+static_assert(TURN_ROWS == ROPE_HALF_ROWS, "the context's fp16 rows");
+constexpr int LOOP_BYTES = (TURN_ROWS * CS_ROW + WARPS * 32) * 16;  // cosines and sines; each warp's next row of the table
+constexpr int MERGE_BYTES = WARPS * Q8_HEADS * O_ROW * 4;
 
 struct Q8AttendParams {
     const uint8_t* k;
@@ -48,6 +55,7 @@ struct Q8AttendParams {
     float* partial;            // [split][batch][kv_heads * g][PART]
     int32_t* tickets;          // [batch * kv_heads * subs], 0 between launches; null: q8_merge_kernel follows
     const float2* table;
+    const uint4* halves;       // its rows 0 .. 63 as fp16: 64 cosines, 64 sines each
     float qscale;              // scale * log2(e)
     int32_t len[ATTEND_MAX_BATCH];
     uint16_t tiles[ATTEND_MAX_BATCH];
@@ -70,6 +78,7 @@ __device__ __forceinline__ void widen(uint32_t w, __half2& a, __half2& b)
     }
 }
 __device__ __forceinline__ uint32_t bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+__device__ __forceinline__ __half2 half2_of(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
 __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
 struct Tile {
@@ -138,16 +147,18 @@ template <int KIND>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const __grid_constant__ Q8AttendParams p)
 {
     wait_for_previous_grid();
-    __shared__ uint4 sm_cs[TILE * CS_ROW];
+    __shared__ __align__(16) uint8_t smem[LOOP_BYTES > MERGE_BYTES ? LOOP_BYTES : MERGE_BYTES];
     __shared__ float4 sm_q[Q8_HEADS * Q_ROW];
-    __shared__ __align__(16) float sm_o[WARPS * Q8_HEADS * O_ROW];
     __shared__ float sm_ml[WARPS][Q8_HEADS][2];
+    uint4* sm_cs = reinterpret_cast<uint4*>(smem);
+    float* sm_o = reinterpret_cast<float*>(smem);  // after the loop
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, gq = lane / 4, tq = lane % 4;
     const int32_t sub = (int32_t)blockIdx.y % p.subs, bh = (int32_t)blockIdx.y / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
     const int32_t len = p.len[b];
     const int32_t rows = p.tiles[b] * TILE, r0 = (int32_t)blockIdx.x * rows, r1 = min(len, r0 + rows);
     if (r0 >= len) return;  // a shorter sequence has fewer splits
-    const int32_t n_tiles = (r1 - r0 + TILE - 1) / TILE;
+    // each warp walks a run of tiles
+    const int32_t n_tiles = (r1 - r0 + TILE - 1) / TILE, per = (n_tiles + WARPS - 1) / WARPS, t0 = min(n_tiles, warp * per), t1 = min(n_tiles, t0 + per);
     const int32_t heads = min(Q8_HEADS, p.g - sub * Q8_HEADS);
     const int64_t bb = p.batch0 + b, head0 = (bb * p.kv_heads + h) * p.g + sub * Q8_HEADS;
     const uint8_t* K = p.k + bb * p.stride_batch + h * p.stride_head + 16 * tq;
@@ -155,23 +166,45 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     const float* KS = p.k_scale + bb * p.scale_batch + (int64_t)h * p.blocks;
     const float* VS = p.v_scale + bb * p.scale_batch + (int64_t)h * p.blocks;
 
-    auto fetch = [&](Tile& t, int32_t tile) {
+    Tile tl;
+    auto fetch_k = [&](int32_t tile) {
         const int32_t j0 = r0 + tile * TILE, last = r1 - 1;  // rows past the end read the last one again; their weights are zero
         const uint8_t* a = K + (int64_t)min(j0 + gq, last) * p.stride_token;
         const uint8_t* c = K + (int64_t)min(j0 + gq + 8, last) * p.stride_token;
-        t.ka_lo = load(reinterpret_cast<const uint4*>(a));
-        t.ka_hi = load(reinterpret_cast<const uint4*>(a + 64));
-        t.kb_lo = load(reinterpret_cast<const uint4*>(c));
-        t.kb_hi = load(reinterpret_cast<const uint4*>(c + 64));
+        tl.ka_lo = load(reinterpret_cast<const uint4*>(a));
+        tl.ka_hi = load(reinterpret_cast<const uint4*>(a + 64));
+        tl.kb_lo = load(reinterpret_cast<const uint4*>(c));
+        tl.kb_hi = load(reinterpret_cast<const uint4*>(c + 64));
+        tl.ks = load1(KS + (j0 >> p.block_shift));
+    };
+    auto fetch_v = [&](int32_t tile) {
+        const int32_t j0 = r0 + tile * TILE, last = r1 - 1;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            t.v[i] = load(reinterpret_cast<const uint4*>(V + (int64_t)min(j0 + 2 * tq + (i & 1) + (i >> 1) * 8, last) * p.stride_token));
-        t.ks = load1(KS + (j0 >> p.block_shift));
-        t.vs = load1(VS + (j0 >> p.block_shift));
+            tl.v[i] = load(reinterpret_cast<const uint4*>(V + (int64_t)min(j0 + 2 * tq + (i & 1) + (i >> 1) * 8, last) * p.stride_token));
+        tl.vs = load1(VS + (j0 >> p.block_shift));
     };
-    Tile cur, nxt;
-    if (warp < n_tiles) fetch(nxt, warp);
-
+    // the row of the table that turns the queries for the four tiles from `tile` on
+    const uint32_t my_turn = (uint32_t)__cvta_generic_to_shared(smem) + (TURN_ROWS * CS_ROW + warp * 32) * 16;
+    auto fetch_turn = [&](int32_t tile) {
+        if (p.table && tile < t1) cp_async16(my_turn + lane * 16, reinterpret_cast<const uint4*>(p.table + (int64_t)(len - 1 - r0 - tile * TILE) * 64) + lane, true);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (t0 < t1) {
+        fetch_k(t0);
+        fetch_v(t0);
+    }
+    // cosines and sines of rows 0 .. 63
+    if (p.table) {
+        for (int i = tid; i < TURN_ROWS * 16; i += THREADS)
+            cp_async16((uint32_t)__cvta_generic_to_shared(sm_cs + i / 16 * CS_ROW + i % 16), p.halves + i, true);
+    } else {
+        for (int i = tid; i < TURN_ROWS * 16; i += THREADS) {
+            const uint32_t x = i % 16 < 8 ? 0x3c003c00u : 0u;  // no RoPE: 1 and 0
+            sm_cs[i / 16 * CS_ROW + i % 16] = make_uint4(x, x, x, x);
+        }
+    }
+    fetch_turn(t0);
     // queries, scaled, before RoPE: lane (gq, tq) reads channels 16 tq + 4 i and 64 + 16 tq + 4 i of head gq at places 4 i + tq, 16 + 4 i + tq
     for (int i = tid; i < Q8_HEADS * 32; i += THREADS) {
         const int head = i / 32, c4 = i % 32, half = c4 / 16, quad = c4 % 16;  // channels 64 half + 4 quad ..
@@ -183,14 +216,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         }
         sm_q[head * Q_ROW + half * 16 + (quad & 3) * 4 + quad / 4] = x;
     }
-    // cosines and sines of rows 0 .. 15
-    for (int i = tid; i < TILE * 64; i += THREADS) {
-        const int r = i / 64, c = i % 64;
-        const float2 cs = p.table ? p.table[i] : make_float2(1.f, 0.f);
-        __half* at = reinterpret_cast<__half*>(sm_cs + r * CS_ROW);
-        at[c] = __float2half_rn(cs.x);
-        at[64 + c] = __float2half_rn(cs.y);
-    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
 
     float m_run[2] = {NEG, NEG}, l_run[2] = {0.f, 0.f}, vref = 0.f, vinv = 0.f;
@@ -199,56 +225,68 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+    uint32_t q_lo[4][2], q_hi[4][2];
 
-    for (int32_t tile = warp; tile < n_tiles; tile += WARPS) {
-        cur = nxt;
-        if (tile + WARPS < n_tiles) fetch(nxt, tile + WARPS);
-        const int32_t j0 = r0 + tile * TILE;
-
-        // scores of rows gq, gq + 8 and heads 2 tq, 2 tq + 1; four channels and their partners a turn
-        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
-        const float4* turn = p.table ? reinterpret_cast<const float4*>(p.table + (int64_t)(len - 1 - j0) * 64 + 16 * tq) : nullptr;
+    for (int32_t tile = t0; tile < t1; ++tile) {
+        const int32_t j0 = r0 + tile * TILE, sub_tile = (tile - t0) % TURN_TILES;
+        if (sub_tile == 0) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            const float4* turn = reinterpret_cast<const float4*>(smem + (TURN_ROWS * CS_ROW + warp * 32) * 16) + 8 * tq;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            uint32_t q_lo[2], q_hi[2];
-            {
+            for (int w = 0; w < 4; ++w) {
                 float4 lo = sm_q[gq * Q_ROW + w * 4 + tq], hi = sm_q[gq * Q_ROW + 16 + w * 4 + tq];
-                if (turn) {
-                    const float4 c0 = __ldg(turn + 2 * w), c1 = __ldg(turn + 2 * w + 1);
+                if (p.table) {
+                    const float4 c0 = turn[2 * w], c1 = turn[2 * w + 1];
                     rotate(lo.x, hi.x, make_float2(c0.x, c0.y));
                     rotate(lo.y, hi.y, make_float2(c0.z, c0.w));
                     rotate(lo.z, hi.z, make_float2(c1.x, c1.y));
                     rotate(lo.w, hi.w, make_float2(c1.z, c1.w));
                 }
-                q_lo[0] = pack2_f16(lo.x, lo.y);
-                q_lo[1] = pack2_f16(lo.z, lo.w);
-                q_hi[0] = pack2_f16(hi.x, hi.y);
-                q_hi[1] = pack2_f16(hi.z, hi.w);
+                q_lo[w][0] = pack2_f16(lo.x, lo.y);
+                q_lo[w][1] = pack2_f16(lo.z, lo.w);
+                q_hi[w][0] = pack2_f16(hi.x, hi.y);
+                q_hi[w][1] = pack2_f16(hi.z, hi.w);
             }
-            uint32_t a_lo[4], a_hi[4];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {  // rows gq, gq + 8
-                __half2 lo[2], hi[2];
-                widen<KIND>(word(r ? cur.kb_lo : cur.ka_lo, w), lo[0], lo[1]);
-                widen<KIND>(word(r ? cur.kb_hi : cur.ka_hi, w), hi[0], hi[1]);
-                const __half2* cs = reinterpret_cast<const __half2*>(sm_cs + (gq + 8 * r) * CS_ROW + 2 * tq) + 2 * w;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const __half2 c = cs[i], s = cs[32 + i];
-                    a_lo[r + 2 * i] = bits(__hfma2(__hneg2(hi[i]), s, __hmul2(lo[i], c)));
-                    a_hi[r + 2 * i] = bits(__hfma2(lo[i], s, __hmul2(hi[i], c)));
-                }
-            }
-            mma_f16(s0, a_lo, q_lo[0], q_lo[1]);
-            mma_f16(s1, a_hi, q_hi[0], q_hi[1]);
+            __syncwarp();
+            fetch_turn(tile + TURN_TILES);
         }
+
+        // scores of rows gq, gq + 8 and heads 2 tq, 2 tq + 1; four channels and their partners a turn
+        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint4* cs_a = sm_cs + (sub_tile * TILE + gq) * CS_ROW + 2 * tq;
+#pragma unroll
+        for (int w2 = 0; w2 < 2; ++w2) {
+            const uint4 ca = cs_a[w2], sa = cs_a[8 + w2], cb = cs_a[8 * CS_ROW + w2], sb = cs_a[8 * CS_ROW + 8 + w2];
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int w = 2 * w2 + v;
+                uint32_t a_lo[4], a_hi[4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {  // rows gq, gq + 8
+                    __half2 lo[2], hi[2];
+                    widen<KIND>(word(r ? tl.kb_lo : tl.ka_lo, w), lo[0], lo[1]);
+                    widen<KIND>(word(r ? tl.kb_hi : tl.ka_hi, w), hi[0], hi[1]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const __half2 c = half2_of(word(r ? cb : ca, 2 * v + i)), sn = half2_of(word(r ? sb : sa, 2 * v + i));
+                        a_lo[r + 2 * i] = bits(__hfma2(__hneg2(hi[i]), sn, __hmul2(lo[i], c)));
+                        a_hi[r + 2 * i] = bits(__hfma2(lo[i], sn, __hmul2(hi[i], c)));
+                    }
+                }
+                mma_f16(s0, a_lo, q_lo[w][0], q_lo[w][1]);
+                mma_f16(s1, a_hi, q_hi[w][0], q_hi[w][1]);
+            }
+        }
+        const float ks = tl.ks;
+        if (tile + 1 < t1) fetch_k(tile + 1);
         // running softmax, this thread's rows gq and gq + 8
         const int32_t left = r1 - j0;
         const bool ok0 = gq < left, ok1 = gq + 8 < left;
         float corr[2], pw[2][2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const float sa = (s0[j] + s1[j]) * cur.ks, sb = (s0[2 + j] + s1[2 + j]) * cur.ks;
+            const float sa = (s0[j] + s1[j]) * ks, sb = (s0[2 + j] + s1[2 + j]) * ks;
             float mx = fmaxf(ok0 ? sa : NEG, ok1 ? sb : NEG);
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
@@ -260,14 +298,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
             pw[1][j] = ok1 ? ex2(sb - m_new) : 0.f;
             l_run[j] = fmaf(l_run[j], corr[j], pw[0][j] + pw[1][j]);
         }
-        if (cur.vs > vref) {  // the weights' unit grows
-            const float f = vref / cur.vs;
+        if (tl.vs > vref) {  // the weights' unit grows
+            const float f = vref / tl.vs;
             corr[0] *= f;
             corr[1] *= f;
-            vref = cur.vs;
+            vref = tl.vs;
             vinv = 1.f / vref;
         }
-        const float unit = cur.vs * vinv;
+        const float unit = tl.vs * vinv;
         if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -282,7 +320,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         // O^T += V^T P: product i takes channels 16 gq + 2 i and + 1
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const uint32_t v0 = word(cur.v[0], w), v1 = word(cur.v[1], w), v2 = word(cur.v[2], w), v3 = word(cur.v[3], w);
+            const uint32_t v0 = word(tl.v[0], w), v1 = word(tl.v[1], w), v2 = word(tl.v[2], w), v3 = word(tl.v[3], w);
             __half2 x[4], y[4];  // channels 4 w + i: rows 2 tq, 2 tq + 1; rows 2 tq + 8, 2 tq + 9
             widen<KIND>(__byte_perm(v0, v1, 0x5140), x[0], x[1]);
             widen<KIND>(__byte_perm(v0, v1, 0x7362), x[2], x[3]);
@@ -294,7 +332,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
                 mma_f16(o[2 * w + i], a, p0, p1);
             }
         }
+        if (tile + 1 < t1) fetch_v(tile + 1);
     }
+    __syncthreads();  // the cosines and sines make room
 
     // merge the warps: channel 16 gq + x at place 8 x + gq, so that a store meets no bank twice
 #pragma unroll
@@ -383,8 +423,8 @@ cudaError_t launch(void (*kernel)(const Q8AttendParams), dim3 grid, const Q8Atte
 int64_t attend_q8_resident(int sm_count) { return (int64_t)sm_count * CTAS_PER_SM; }
 
 cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, const void* q, void* out, int32_t g, const int32_t* lens,
-                             const float2* table, float scale, const AttendPlan& plan, float* partial, int32_t* tickets,
-                             int32_t* launched, cudaStream_t stream)
+                             const float2* table, const uint4* halves, float scale, const AttendPlan& plan, float* partial,
+                             int32_t* tickets, int32_t* launched, cudaStream_t stream)
 {
     *launched = 0;
     Q8AttendParams prm;
@@ -409,6 +449,7 @@ cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, 
     // (a captured launch takes no tickets and does not overlap the one before: see launch_attend)
     prm.tickets = plan.one_wave && !plan.captured ? tickets : nullptr;
     prm.table = table;
+    prm.halves = halves;
     prm.qscale = scale * 1.4426950408889634f;
     // sequences per launch: their lengths travel as kernel arguments, their groups are rows of the grid
     const int32_t groups = cache.kv_heads * prm.subs, per_launch = std::max(1, std::min(ATTEND_MAX_BATCH, 65535 / groups));
