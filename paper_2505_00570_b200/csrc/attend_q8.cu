@@ -3,10 +3,11 @@
 //
 // One pass over the codes of the layer, 256 bytes a row of K and V: bound by memory, and at the copy rate an SM has 11 clocks
 // for a row, so what counts next to the loads is the instructions a row takes.  A warp takes tiles of 16 rows:
-//  - Codes go from memory into registers in the layout that the matrix instruction (mma.sync m16n8k16, fp32 accumulation) wants,
-//    without shared memory.  The order of the contraction index is free, so a lane's share of a key row is 16 consecutive
-//    channels and the 16 that RoPE pairs with them (two 16-byte loads), and its share of four value rows is 16 channels each.
-//    A tile's keys make room for the next one's as soon as its scores are there, its values after the second product.
+//  - The next tile is on its way into the warp's own two-stage ring in shared memory (cp.async) while a tile is computed.
+//    From there codes go into registers as the matrix instruction (mma.sync m16n8k16, fp32 accumulation) wants them: the order of
+//    the contraction index is free, so a lane's share of a key row is 16 consecutive channels and the 16 that RoPE pairs
+//    with them, and its share of four value rows is 16 channels each, eight 16-byte reads in all, at swizzled places
+//    that meet no bank twice.
 //  - Codes become fp16 exactly (e4m3: one conversion of two; int8: a byte permute and a subtraction of two).  For V, whose rows are
 //    the contraction index, the bytes of two rows are interleaved before the conversion.
 //  - RoPE: the score of key row j0 + r and the query at len - 1 is  k . R(len - 1 - j0 - r) q, and is computed as
@@ -30,7 +31,7 @@
 namespace freqkv {
 namespace {
 
-constexpr int WARPS = 4, THREADS = 32 * WARPS, CTAS_PER_SM = 4;
+constexpr int WARPS = 8, THREADS = 32 * WARPS, CTAS_PER_SM = 2;
 static_assert(CTAS_PER_SM <= ATTEND_MOST_CTAS_PER_SM, "tickets");
 constexpr int TILE = 16;
 constexpr int TURN_TILES = 4;                 // tiles whose queries are turned alike
@@ -39,8 +40,11 @@ constexpr int CS_ROW = 17;   // uint4 per row of the cosines and sines: 8 + 8, a
 constexpr int Q_ROW = 36;    // float4 per head: 32, and 4 likewise
 constexpr int O_ROW = 132;   // floats per head of the warps' merge
 static_assert(TURN_ROWS == ROPE_HALF_ROWS, "the context's fp16 rows");
-constexpr int LOOP_BYTES = (TURN_ROWS * CS_ROW + WARPS * 32) * 16;  // cosines and sines; each warp's next row of the table
-constexpr int MERGE_BYTES = WARPS * Q8_HEADS * O_ROW * 4;
+constexpr int STAGES = 2, TILE_BYTES = TILE * 128, STAGE_BYTES = 2 * TILE_BYTES;  // K and V
+constexpr int OFF_CS = WARPS * STAGES * STAGE_BYTES, OFF_TURN = OFF_CS + TURN_ROWS * CS_ROW * 16, OFF_Q = OFF_TURN + WARPS * 512;
+constexpr int SMEM_BYTES = OFF_Q + Q8_HEADS * Q_ROW * 16;
+static_assert(WARPS * Q8_HEADS * O_ROW * 4 <= OFF_CS, "the merge of the warps reuses the ring");
+static_assert(2 * (SMEM_BYTES + 2048) <= 233472, "two CTAs per SM");
 
 struct Q8AttendParams {
     const uint8_t* k;
@@ -78,14 +82,14 @@ __device__ __forceinline__ void widen(uint32_t w, __half2& a, __half2& b)
     }
 }
 __device__ __forceinline__ uint32_t bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
+__device__ __forceinline__ uint4 lds16(const uint8_t* p) { return *reinterpret_cast<const uint4*>(p); }
 __device__ __forceinline__ __half2 half2_of(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
 __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
 
-struct Tile {
-    uint4 ka_lo, ka_hi, kb_lo, kb_hi;  // rows gq and gq + 8: channels 16 tq .. and 64 + 16 tq ..
-    uint4 v[4];                        // rows 2 tq, 2 tq + 1, 2 tq + 8, 2 tq + 9: channels 16 gq ..
-    float ks, vs;                      // the block's scales
-};
+// Where the 16-byte chunk ch of row r of a K or V tile lies.  K: lanes (gq, tq) read chunks tq and 4 + tq of rows gq; V: chunks gq of
+// rows 2 tq + const.  Eight neighbouring lanes then find their chunks in different banks.
+__device__ __forceinline__ uint32_t k_place(int r, int ch) { return (uint32_t)(r * 128 + ((ch ^ ((r & 1) << 2)) << 4)); }
+__device__ __forceinline__ uint32_t v_place(int r, int ch) { return (uint32_t)(r * 128 + ((ch ^ (r & 6)) << 4)); }
 
 // Channel of place t in the partial results: lanes of equal tq write neighbours, see the merge of the warps.
 __device__ __forceinline__ int channel_of(int t) { return (t & 7) * 16 + (t >> 3); }
@@ -95,7 +99,8 @@ __device__ __forceinline__ int channel_of(int t) { return (t & 7) * 16 + (t >> 3
 __device__ __forceinline__ void q8_merge(const Q8AttendParams& p, int64_t head0, int32_t heads, int32_t n_splits, float* sm)
 {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int32_t per = heads >= WARPS ? 1 : heads == 1 ? WARPS : WARPS / 2;  // warps a head; with 3 heads, 2 and two rounds
+    const int32_t per = heads > 4 ? 1 : heads > 2 ? 2 : heads > 1 ? 4 : 8;  // warps a head
+    static_assert(WARPS == 8, "warps a head");
     const int64_t heads_total = (int64_t)p.total_batch * p.kv_heads * p.g;
     for (int32_t g0 = 0; g0 < heads; g0 += WARPS / per) {
         const int32_t g = g0 + warp / per;
@@ -143,14 +148,15 @@ __device__ __forceinline__ void q8_merge(const Q8AttendParams& p, int64_t head0,
     }
 }
 
-template <int KIND>
+// DENSE: rows follow one another.
+template <int KIND, bool DENSE>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const __grid_constant__ Q8AttendParams p)
 {
     wait_for_previous_grid();
-    __shared__ __align__(16) uint8_t smem[LOOP_BYTES > MERGE_BYTES ? LOOP_BYTES : MERGE_BYTES];
-    __shared__ float4 sm_q[Q8_HEADS * Q_ROW];
+    extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float sm_ml[WARPS][Q8_HEADS][2];
-    uint4* sm_cs = reinterpret_cast<uint4*>(smem);
+    uint4* sm_cs = reinterpret_cast<uint4*>(smem + OFF_CS);
+    float4* sm_q = reinterpret_cast<float4*>(smem + OFF_Q);
     float* sm_o = reinterpret_cast<float*>(smem);  // after the loop
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, gq = lane / 4, tq = lane % 4;
     const int32_t sub = (int32_t)blockIdx.y % p.subs, bh = (int32_t)blockIdx.y / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
@@ -161,39 +167,45 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     const int32_t n_tiles = (r1 - r0 + TILE - 1) / TILE, per = (n_tiles + WARPS - 1) / WARPS, t0 = min(n_tiles, warp * per), t1 = min(n_tiles, t0 + per);
     const int32_t heads = min(Q8_HEADS, p.g - sub * Q8_HEADS);
     const int64_t bb = p.batch0 + b, head0 = (bb * p.kv_heads + h) * p.g + sub * Q8_HEADS;
-    const uint8_t* K = p.k + bb * p.stride_batch + h * p.stride_head + 16 * tq;
-    const uint8_t* V = p.v + bb * p.stride_batch + h * p.stride_head + 16 * gq;
+    const uint8_t* K = p.k + bb * p.stride_batch + h * p.stride_head;
+    const uint8_t* V = p.v + bb * p.stride_batch + h * p.stride_head;
     const float* KS = p.k_scale + bb * p.scale_batch + (int64_t)h * p.blocks;
     const float* VS = p.v_scale + bb * p.scale_batch + (int64_t)h * p.blocks;
 
-    Tile tl;
-    auto fetch_k = [&](int32_t tile) {
-        const int32_t j0 = r0 + tile * TILE, last = r1 - 1;  // rows past the end read the last one again; their weights are zero
-        const uint8_t* a = K + (int64_t)min(j0 + gq, last) * p.stride_token;
-        const uint8_t* c = K + (int64_t)min(j0 + gq + 8, last) * p.stride_token;
-        tl.ka_lo = load(reinterpret_cast<const uint4*>(a));
-        tl.ka_hi = load(reinterpret_cast<const uint4*>(a + 64));
-        tl.kb_lo = load(reinterpret_cast<const uint4*>(c));
-        tl.kb_hi = load(reinterpret_cast<const uint4*>(c + 64));
-        tl.ks = load1(KS + (j0 >> p.block_shift));
-    };
-    auto fetch_v = [&](int32_t tile) {
-        const int32_t j0 = r0 + tile * TILE, last = r1 - 1;
+    const int32_t warp_end = min(r1, r0 + t1 * TILE);
+    // Lane (lane / 8, lane % 8) copies chunk lane % 8 of rows lane / 8 + 4 i.  One group is committed per tile, empty past the last.
+    uint8_t* ring = smem + warp * (STAGES * STAGE_BYTES);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const int64_t pitch = DENSE ? 128 : p.stride_token;  // DENSE: the rows of a tile lie at offsets that the copies hold
+    auto fetch = [&](int32_t tile, int stage) {
+        if (tile < t1) {
+            const int32_t j0 = r0 + tile * TILE, row = lane >> 3, ch = lane & 7;
+            const uint32_t at = ring_at + stage * STAGE_BYTES;
+            if (j0 + TILE <= warp_end) {
+                const int64_t off = (j0 + row) * pitch + ch * 16;
+                const uint8_t *k0 = K + off, *v0 = V + off;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            tl.v[i] = load(reinterpret_cast<const uint4*>(V + (int64_t)min(j0 + 2 * tq + (i & 1) + (i >> 1) * 8, last) * p.stride_token));
-        tl.vs = load1(VS + (j0 >> p.block_shift));
+                for (int i = 0; i < 4; ++i) {
+                    cp_async16(at + k_place(row + 4 * i, ch), k0 + 4 * i * pitch, true);
+                    cp_async16(at + TILE_BYTES + v_place(row + 4 * i, ch), v0 + 4 * i * pitch, true);
+                }
+            } else {  // rows past the end: zeros, whose scores are masked
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool there = j0 + row + 4 * i < warp_end;
+                    const int64_t off = (there ? j0 + row + 4 * i : j0) * pitch + ch * 16;
+                    cp_async16(at + k_place(row + 4 * i, ch), K + off, there);
+                    cp_async16(at + TILE_BYTES + v_place(row + 4 * i, ch), V + off, there);
+                }
+            }
+        }
     };
     // the row of the table that turns the queries for the four tiles from `tile` on
-    const uint32_t my_turn = (uint32_t)__cvta_generic_to_shared(smem) + (TURN_ROWS * CS_ROW + warp * 32) * 16;
+    const uint32_t my_turn = (uint32_t)__cvta_generic_to_shared(smem) + OFF_TURN + warp * 512;
     auto fetch_turn = [&](int32_t tile) {
         if (p.table && tile < t1) cp_async16(my_turn + lane * 16, reinterpret_cast<const uint4*>(p.table + (int64_t)(len - 1 - r0 - tile * TILE) * 64) + lane, true);
-        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (t0 < t1) {
-        fetch_k(t0);
-        fetch_v(t0);
-    }
+    fetch(t0, 0);
     // cosines and sines of rows 0 .. 63
     if (p.table) {
         for (int i = tid; i < TURN_ROWS * 16; i += THREADS)
@@ -216,6 +228,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         }
         sm_q[head * Q_ROW + half * 16 + (quad & 3) * 4 + quad / 4] = x;
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
 
@@ -227,12 +240,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
     uint32_t q_lo[4][2], q_hi[4][2];
 
-    for (int32_t tile = t0; tile < t1; ++tile) {
+    int stage = 0;
+    for (int32_t tile = t0; tile < t1; ++tile, stage ^= 1) {
         const int32_t j0 = r0 + tile * TILE, sub_tile = (tile - t0) % TURN_TILES;
+        const float ks = load1(KS + (j0 >> p.block_shift)), vs = load1(VS + (j0 >> p.block_shift));
+        __syncwarp();  // every lane is done with the stage that is filled now
+        fetch(tile + 1, stage ^ 1);
         if (sub_tile == 0) {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            __syncwarp();
-            const float4* turn = reinterpret_cast<const float4*>(smem + (TURN_ROWS * CS_ROW + warp * 32) * 16) + 8 * tq;
+            const float4* turn = reinterpret_cast<const float4*>(smem + OFF_TURN + warp * 512) + 8 * tq;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 float4 lo = sm_q[gq * Q_ROW + w * 4 + tq], hi = sm_q[gq * Q_ROW + 16 + w * 4 + tq];
@@ -249,63 +264,70 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
                 q_hi[w][1] = pack2_f16(hi.z, hi.w);
             }
             __syncwarp();
-            fetch_turn(tile + TURN_TILES);
+            fetch_turn(tile + TURN_TILES);  // (with the next tile's group: there before it is read, three tiles on)
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        const uint8_t* kt = ring + stage * STAGE_BYTES;
+        const uint8_t* vt = kt + TILE_BYTES;
 
         // scores of rows gq, gq + 8 and heads 2 tq, 2 tq + 1; four channels and their partners a turn
         float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
-        const uint4* cs_a = sm_cs + (sub_tile * TILE + gq) * CS_ROW + 2 * tq;
+        {
+            const uint4 k_lo[2] = {lds16(kt + k_place(gq, tq)), lds16(kt + k_place(gq + 8, tq))};
+            const uint4 k_hi[2] = {lds16(kt + k_place(gq, 4 + tq)), lds16(kt + k_place(gq + 8, 4 + tq))};
+            const uint4* cs = sm_cs + (sub_tile * TILE + gq) * CS_ROW + 2 * tq;
 #pragma unroll
-        for (int w2 = 0; w2 < 2; ++w2) {
-            const uint4 ca = cs_a[w2], sa = cs_a[8 + w2], cb = cs_a[8 * CS_ROW + w2], sb = cs_a[8 * CS_ROW + 8 + w2];
+            for (int w2 = 0; w2 < 2; ++w2) {
+                const uint4 c[2] = {cs[w2], cs[8 * CS_ROW + w2]}, sn[2] = {cs[8 + w2], cs[8 * CS_ROW + 8 + w2]};
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int w = 2 * w2 + v;
-                uint32_t a_lo[4], a_hi[4];
+                for (int v = 0; v < 2; ++v) {
+                    const int w = 2 * w2 + v;
+                    uint32_t a_lo[4], a_hi[4];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {  // rows gq, gq + 8
-                    __half2 lo[2], hi[2];
-                    widen<KIND>(word(r ? tl.kb_lo : tl.ka_lo, w), lo[0], lo[1]);
-                    widen<KIND>(word(r ? tl.kb_hi : tl.ka_hi, w), hi[0], hi[1]);
+                    for (int r = 0; r < 2; ++r) {  // rows gq, gq + 8
+                        __half2 lo[2], hi[2];
+                        widen<KIND>(word(k_lo[r], w), lo[0], lo[1]);
+                        widen<KIND>(word(k_hi[r], w), hi[0], hi[1]);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const __half2 c = half2_of(word(r ? cb : ca, 2 * v + i)), sn = half2_of(word(r ? sb : sa, 2 * v + i));
-                        a_lo[r + 2 * i] = bits(__hfma2(__hneg2(hi[i]), sn, __hmul2(lo[i], c)));
-                        a_hi[r + 2 * i] = bits(__hfma2(lo[i], sn, __hmul2(hi[i], c)));
+                        for (int i = 0; i < 2; ++i) {
+                            const __half2 cc = half2_of(word(c[r], 2 * v + i)), ss = half2_of(word(sn[r], 2 * v + i));
+                            a_lo[r + 2 * i] = bits(__hfma2(__hneg2(hi[i]), ss, __hmul2(lo[i], cc)));
+                            a_hi[r + 2 * i] = bits(__hfma2(lo[i], ss, __hmul2(hi[i], cc)));
+                        }
                     }
+                    mma_f16(s0, a_lo, q_lo[w][0], q_lo[w][1]);
+                    mma_f16(s1, a_hi, q_hi[w][0], q_hi[w][1]);
                 }
-                mma_f16(s0, a_lo, q_lo[w][0], q_lo[w][1]);
-                mma_f16(s1, a_hi, q_hi[w][0], q_hi[w][1]);
             }
         }
-        const float ks = tl.ks;
-        if (tile + 1 < t1) fetch_k(tile + 1);
         // running softmax, this thread's rows gq and gq + 8
-        const int32_t left = r1 - j0;
-        const bool ok0 = gq < left, ok1 = gq + 8 < left;
         float corr[2], pw[2][2];
 #pragma unroll
+        for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = (s0[i] + s1[i]) * ks;
+        if (j0 + TILE > warp_end) {
+            if (j0 + gq >= warp_end) pw[0][0] = pw[0][1] = -INFINITY;
+            if (j0 + gq + 8 >= warp_end) pw[1][0] = pw[1][1] = -INFINITY;
+        }
+#pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const float sa = (s0[j] + s1[j]) * ks, sb = (s0[2 + j] + s1[2 + j]) * ks;
-            float mx = fmaxf(ok0 ? sa : NEG, ok1 ? sb : NEG);
+            float mx = fmaxf(m_run[j], fmaxf(pw[0][j], pw[1][j]));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
             mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            const float m_new = fmaxf(m_run[j], mx);
-            corr[j] = ex2(m_run[j] - m_new);
-            m_run[j] = m_new;
-            pw[0][j] = ok0 ? ex2(sa - m_new) : 0.f;
-            pw[1][j] = ok1 ? ex2(sb - m_new) : 0.f;
+            corr[j] = ex2(m_run[j] - mx);
+            m_run[j] = mx;
+            pw[0][j] = ex2(pw[0][j] - mx);
+            pw[1][j] = ex2(pw[1][j] - mx);
             l_run[j] = fmaf(l_run[j], corr[j], pw[0][j] + pw[1][j]);
         }
-        if (tl.vs > vref) {  // the weights' unit grows
-            const float f = vref / tl.vs;
+        if (vs > vref) {  // the weights' unit grows
+            const float f = vref / vs;
             corr[0] *= f;
             corr[1] *= f;
-            vref = tl.vs;
+            vref = vs;
             vinv = 1.f / vref;
         }
-        const float unit = tl.vs * vinv;
+        const float unit = vs * vinv;
         if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -318,9 +340,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         const uint32_t p0 = transpose_8x8(pack2_f16(pw[0][0] * unit, pw[0][1] * unit));
         const uint32_t p1 = transpose_8x8(pack2_f16(pw[1][0] * unit, pw[1][1] * unit));
         // O^T += V^T P: product i takes channels 16 gq + 2 i and + 1
+        const uint4 v[4] = {lds16(vt + v_place(2 * tq, gq)), lds16(vt + v_place(2 * tq + 1, gq)), lds16(vt + v_place(2 * tq + 8, gq)),
+                            lds16(vt + v_place(2 * tq + 9, gq))};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const uint32_t v0 = word(tl.v[0], w), v1 = word(tl.v[1], w), v2 = word(tl.v[2], w), v3 = word(tl.v[3], w);
+            const uint32_t v0 = word(v[0], w), v1 = word(v[1], w), v2 = word(v[2], w), v3 = word(v[3], w);
             __half2 x[4], y[4];  // channels 4 w + i: rows 2 tq, 2 tq + 1; rows 2 tq + 8, 2 tq + 9
             widen<KIND>(__byte_perm(v0, v1, 0x5140), x[0], x[1]);
             widen<KIND>(__byte_perm(v0, v1, 0x7362), x[2], x[3]);
@@ -332,9 +356,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
                 mma_f16(o[2 * w + i], a, p0, p1);
             }
         }
-        if (tile + 1 < t1) fetch_v(tile + 1);
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
-    __syncthreads();  // the cosines and sines make room
+    __syncthreads();  // the ring makes room
 
     // merge the warps: channel 16 gq + x at place 8 x + gq, so that a store meets no bank twice
 #pragma unroll
@@ -356,7 +380,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     }
     __syncthreads();
     const int32_t n_splits = (len + rows - 1) / rows;
-    for (int32_t g = 0; g < heads; ++g) {
+    const int c = tid % 128;
+    for (int32_t g = tid / 128; g < heads; g += THREADS / 128) {
         float mn = NEG, sum = 0.f, acc = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) mn = fmaxf(mn, sm_ml[w][g][0]);
@@ -364,15 +389,15 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         for (int w = 0; w < WARPS; ++w) {
             const float f = ex2(sm_ml[w][g][0] - mn);
             sum = fmaf(sm_ml[w][g][1], f, sum);
-            acc = fmaf(sm_o[(w * Q8_HEADS + g) * O_ROW + tid], f, acc);
+            acc = fmaf(sm_o[(w * Q8_HEADS + g) * O_ROW + c], f, acc);
         }
         if (n_splits == 1) {
-            p.out[(head0 + g) * 128 + channel_of(tid)] = __float2bfloat16_rn(acc / sum);
+            p.out[(head0 + g) * 128 + channel_of(c)] = __float2bfloat16_rn(acc / sum);
             continue;
         }
         float* part = p.partial + (((int64_t)blockIdx.x * p.total_batch + bb) * p.kv_heads * p.g + h * p.g + sub * Q8_HEADS + g) * PART;
-        part[4 + tid] = acc;
-        if (tid == 0) {
+        part[4 + c] = acc;
+        if (c == 0) {
             part[0] = mn;
             part[1] = sum;
         }
@@ -404,11 +429,12 @@ __global__ void __launch_bounds__(THREADS) q8_merge_kernel(const __grid_constant
     q8_merge(p, ((int64_t)(p.batch0 + b) * p.kv_heads + h) * p.g + sub * Q8_HEADS, min(Q8_HEADS, p.g - sub * Q8_HEADS), n_splits, sm);
 }
 
-cudaError_t launch(void (*kernel)(const Q8AttendParams), dim3 grid, const Q8AttendParams& prm, bool overlap, cudaStream_t stream)
+cudaError_t launch(void (*kernel)(const Q8AttendParams), dim3 grid, int smem, const Q8AttendParams& prm, bool overlap, cudaStream_t stream)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -427,6 +453,17 @@ cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, 
                              int32_t* tickets, int32_t* launched, cudaStream_t stream)
 {
     *launched = 0;
+    static PerDeviceOnce attrs;
+    const cudaError_t attr_error = attrs.run([] {
+        for (const void* f : {(const void*)attend_q8_kernel<FREQKV_Q8_INT8, true>, (const void*)attend_q8_kernel<FREQKV_Q8_E4M3, true>,
+                              (const void*)attend_q8_kernel<FREQKV_Q8_INT8, false>, (const void*)attend_q8_kernel<FREQKV_Q8_E4M3, false>}) {
+            cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+            if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+    });
+    if (attr_error != cudaSuccess) return attr_error;
     Q8AttendParams prm;
     const int64_t scale_layer = (int64_t)layer * cache.kv_heads * cache.blocks;
     prm.k = static_cast<const uint8_t*>(cache.codes[0]) + layer * cache.stride_layer;
@@ -463,12 +500,14 @@ cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, 
             prm.tiles[i] = (uint16_t)(((len + n - 1) / n + 15) / 16);
             splits = std::max(splits, n);
         }
-        const cudaError_t e = launch(cache.kind == FREQKV_Q8_INT8 ? attend_q8_kernel<FREQKV_Q8_INT8> : attend_q8_kernel<FREQKV_Q8_E4M3>,
-                                     dim3((unsigned)splits, (unsigned)(nb * groups)), prm, !plan.captured, stream);
+        const bool dense = cache.stride_token == 128, int8 = cache.kind == FREQKV_Q8_INT8;
+        const cudaError_t e = launch(dense ? (int8 ? attend_q8_kernel<FREQKV_Q8_INT8, true> : attend_q8_kernel<FREQKV_Q8_E4M3, true>)
+                                           : (int8 ? attend_q8_kernel<FREQKV_Q8_INT8, false> : attend_q8_kernel<FREQKV_Q8_E4M3, false>),
+                                     dim3((unsigned)splits, (unsigned)(nb * groups)), SMEM_BYTES, prm, !plan.captured, stream);
         if (e != cudaSuccess) return e;
         ++*launched;
         if (!prm.tickets && splits > 1) {
-            const cudaError_t me = launch(q8_merge_kernel, dim3((unsigned)(nb * groups)), prm, true, stream);
+            const cudaError_t me = launch(q8_merge_kernel, dim3((unsigned)(nb * groups)), 0, prm, true, stream);
             if (me != cudaSuccess) return me;
             ++*launched;
         }
