@@ -159,6 +159,7 @@ def dtype_code(dtype: torch.dtype) -> int:
 
 
 _layout_cache: dict = {}
+_q8_layout_cache: dict = {}
 
 
 def layout_of(t: torch.Tensor) -> Layout:
@@ -259,6 +260,23 @@ class Q8Cache:
     ``k_scale``, ``v_scale`` [batch, layers, kv_heads, ceil(capacity / block_tokens)]."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_tokens: int):
+        # layouts are checked once: a decode loop may wrap the same tensors every step
+        key = (k.dtype, k.shape, k.stride(), v.dtype, v.shape, v.stride(), k_scale.dtype, k_scale.shape, k_scale.stride(),
+               v_scale.dtype, v_scale.shape, v_scale.stride(), block_tokens)
+        ref = _q8_layout_cache.get(key)
+        if ref is None:
+            ref = self._check(k, v, k_scale, v_scale, block_tokens)
+            if len(_q8_layout_cache) > 256:
+                _q8_layout_cache.clear()
+            _q8_layout_cache[key] = ref
+        if not k.device == v.device == k_scale.device == v_scale.device:
+            raise FreqKVError(ERR_INVALID_ARG, "codes and scales must be on one device")
+        self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
+        self.layout, self._ref = ref
+        self._ptrs = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    @staticmethod
+    def _check(k, v, k_scale, v_scale, block_tokens):
         kinds = {torch.float8_e4m3fn: Q8_E4M3, torch.int8: Q8_INT8}
         if k.dtype not in kinds:
             raise FreqKVError(ERR_UNSUPPORTED, f"unsupported code type {k.dtype}")
@@ -270,12 +288,10 @@ class Q8Cache:
             raise FreqKVError(ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128")
         want = (*k.shape[:3], -(-k.shape[3] // block_tokens))
         for s in (k_scale, v_scale):
-            if s.dtype != torch.float32 or tuple(s.shape) != want or not s.is_contiguous() or s.device != k.device:
-                raise FreqKVError(ERR_INVALID_ARG, f"scales must be dense fp32 {want} on the codes' device")
-        self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
-        self.layout = Q8Layout(kinds[k.dtype], *k.shape, block_tokens, *k.stride()[:4])
-        self._ref = ctypes.byref(self.layout)
-        self._ptrs = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+            if s.dtype != torch.float32 or tuple(s.shape) != want or not s.is_contiguous():
+                raise FreqKVError(ERR_INVALID_ARG, f"scales must be dense fp32 {want}")
+        layout = Q8Layout(kinds[k.dtype], *k.shape, block_tokens, *k.stride()[:4])
+        return layout, ctypes.byref(layout)
 
     @classmethod
     def empty(cls, batch: int, layers: int, kv_heads: int, capacity: int, head_dim: int = 128, kind: int = Q8_E4M3,

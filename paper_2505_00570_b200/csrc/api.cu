@@ -89,14 +89,15 @@ freqkv_status check_layout(const freqkv_layout* l)
     }
     // No two matrices may overlap: ordered by stride, each axis must step over the whole extent
     // of the axes below it (axes of extent 1 never step).
-    std::vector<std::pair<int64_t, int64_t>> axes;  // (stride, extent)
+    std::pair<int64_t, int64_t> axes[4];  // (stride, extent)
+    int n_axes = 0;
     for (int i = 0; i < 4; ++i)
-        if (extents[i] > 1) axes.emplace_back(strides[i], extents[i]);
-    std::sort(axes.begin(), axes.end());
+        if (extents[i] > 1) axes[n_axes++] = {strides[i], extents[i]};
+    std::sort(axes, axes + n_axes);
     int64_t below = l->head_dim;
-    for (const auto& a : axes) {
-        if (a.first < below) return FREQKV_ERR_UNSUPPORTED;
-        below = a.first * a.second;
+    for (int i = 0; i < n_axes; ++i) {
+        if (axes[i].first < below) return FREQKV_ERR_UNSUPPORTED;
+        below = axes[i].first * axes[i].second;
     }
     if (l->stride_token < l->head_dim && l->capacity > 1) return FREQKV_ERR_UNSUPPORTED;
     return FREQKV_OK;
@@ -132,6 +133,15 @@ freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base,
         ctx->rope_rows = rows;
         ctx->rope_base = (double)rope_base;
         ctx->kernels_launched += 1;
+        ctx->rope_settled = false;
+        if (!ctx->rope_made && cudaEventCreateWithFlags(&ctx->rope_made, cudaEventDisableTiming) != cudaSuccess) {
+            ctx->rope_made = nullptr;
+            cudaGetLastError();
+        }
+        if (ctx->rope_made) FREQKV_CUDA(ctx, cudaEventRecord(ctx->rope_made, stream));
+    } else if (!ctx->rope_settled && ctx->rope_made && !is_capturing(stream)) {
+        ctx->rope_settled = cudaEventQuery(ctx->rope_made) == cudaSuccess;
+        if (!ctx->rope_settled) cudaGetLastError();  // not ready is no failure
     }
     *table = ctx->rope_table;
     return FREQKV_OK;
@@ -703,6 +713,7 @@ freqkv_status freqkv_destroy(freqkv_ctx* ctx)
         if (ctx->stage[i]) cudaFree(ctx->stage[i]);
     if (ctx->work_done) cudaEventDestroy(ctx->work_done);
     if (ctx->rope_table) cudaFree(ctx->rope_table);
+    if (ctx->rope_made) cudaEventDestroy(ctx->rope_made);
     if (ctx->attend_work) cudaFree(ctx->attend_work);
     std::free(ctx->attend_lens);
     if (ctx->prefill_keys) cudaFree(ctx->prefill_keys);

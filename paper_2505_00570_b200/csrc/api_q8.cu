@@ -238,7 +238,7 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
     {
         TransformTimer timer(ctx, stream);
         e = launch_attend_q8(q8_view(l, k, v, k_scale, v_scale), l.batch, layer, q, out, q_heads_per_kv, lens, table,
-                             table ? reinterpret_cast<const uint4*>(table + (int64_t)ctx->rope_rows * 64) : nullptr, scale, plan, work.partial,
+                             table ? reinterpret_cast<const uint4*>(table + (int64_t)ctx->rope_rows * 64) : nullptr, ctx->rope_settled, scale, plan, work.partial,
                              work.tickets, &launched, stream);
     }
     ctx->kernels_launched += launched;

@@ -60,6 +60,7 @@ struct Q8AttendParams {
     int32_t* tickets;          // [batch * kv_heads * subs], 0 between launches; null: q8_merge_kernel follows
     const float2* table;
     const uint4* halves;       // its rows 0 .. 63 as fp16: 64 cosines, 64 sines each
+    int32_t early;             // the table's making is known to be over
     float qscale;              // scale * log2(e)
     int32_t len[ATTEND_MAX_BATCH];
     uint16_t tiles[ATTEND_MAX_BATCH];
@@ -96,7 +97,7 @@ __device__ __forceinline__ int channel_of(int t) { return (t & 7) * 16 + (t >> 3
 
 // All splits of the heads of one CTA's group are there: merge them.  Warps share the heads, and the splits of a head where there
 // are fewer heads than warps.  `sm`: WARPS * (128 + 2) floats.
-__device__ __forceinline__ void q8_merge(const Q8AttendParams& p, int64_t head0, int32_t heads, int32_t n_splits, float* sm)
+__device__ __noinline__ void q8_merge(const Q8AttendParams& p, int64_t head0, int32_t heads, int32_t n_splits, float* sm)
 {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int32_t per = heads > 4 ? 1 : heads > 2 ? 2 : heads > 1 ? 4 : 8;  // warps a head
@@ -108,32 +109,58 @@ __device__ __forceinline__ void q8_merge(const Q8AttendParams& p, int64_t head0,
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         if (g < heads) {
             const float* base = p.partial + (head0 + g) * PART;
-            for (int s = lane; s < n_splits; s += 32) mx = fmaxf(mx, __ldcg(base + s * heads_total * PART));
+            constexpr int AHEAD = 4;  // splits whose loads are under way together
+            for (int s0 = warp % per; s0 < n_splits; s0 += AHEAD * per) {
+                float2 ml[AHEAD];
+                float4 o[AHEAD];
 #pragma unroll
-            for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-#pragma unroll 8
-            for (int s = warp % per; s < n_splits; s += per) {
-                const float* pp = base + s * heads_total * PART;
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(pp));
-                const float4 o = __ldcg(reinterpret_cast<const float4*>(pp + 4) + lane);
-                const float f = ex2(ml.x - mx);
-                sum = fmaf(ml.y, f, sum);
-                acc.x = fmaf(o.x, f, acc.x);
-                acc.y = fmaf(o.y, f, acc.y);
-                acc.z = fmaf(o.z, f, acc.z);
-                acc.w = fmaf(o.w, f, acc.w);
+                for (int i = 0; i < AHEAD; ++i) {
+                    const int s = s0 + i * per;
+                    ml[i] = make_float2(NEG, 0.f);
+                    o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (s < n_splits) {
+                        const float* pp = base + s * heads_total * PART;
+                        ml[i] = __ldcg(reinterpret_cast<const float2*>(pp));
+                        o[i] = __ldcg(reinterpret_cast<const float4*>(pp + 4) + lane);
+                    }
+                }
+                float m_new = mx;
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) m_new = fmaxf(m_new, ml[i].x);
+                const float f0 = ex2(mx - m_new);
+                mx = m_new;
+                sum *= f0;
+                acc.x *= f0; acc.y *= f0; acc.z *= f0; acc.w *= f0;
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) {
+                    const float f = ex2(ml[i].x - mx);
+                    sum = fmaf(ml[i].y, f, sum);
+                    acc.x = fmaf(o[i].x, f, acc.x);
+                    acc.y = fmaf(o[i].y, f, acc.y);
+                    acc.z = fmaf(o[i].z, f, acc.z);
+                    acc.w = fmaf(o[i].w, f, acc.w);
+                }
             }
         }
         if (per > 1) {
             float* mine = sm + warp * 132;
             reinterpret_cast<float4*>(mine)[lane] = acc;
-            if (lane == 0) mine[128] = sum;
+            if (lane == 0) {
+                mine[128] = sum;
+                mine[129] = mx;
+            }
             __syncthreads();
             if (warp % per == 0)
                 for (int w = 1; w < per; ++w) {
-                    const float4 other = reinterpret_cast<const float4*>(sm + (warp + w) * 132)[lane];
-                    acc.x += other.x; acc.y += other.y; acc.z += other.z; acc.w += other.w;
-                    sum += sm[(warp + w) * 132 + 128];
+                    const float* theirs = sm + (warp + w) * 132;
+                    const float4 other = reinterpret_cast<const float4*>(theirs)[lane];
+                    const float m_new = fmaxf(mx, theirs[129]), f0 = ex2(mx - m_new), f1 = ex2(theirs[129] - m_new);
+                    mx = m_new;
+                    sum = sum * f0 + theirs[128] * f1;
+                    acc.x = acc.x * f0 + other.x * f1;
+                    acc.y = acc.y * f0 + other.y * f1;
+                    acc.z = acc.z * f0 + other.z * f1;
+                    acc.w = acc.w * f0 + other.w * f1;
                 }
             __syncthreads();
         }
@@ -152,13 +179,24 @@ __device__ __forceinline__ void q8_merge(const Q8AttendParams& p, int64_t head0,
 template <int KIND, bool DENSE>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const __grid_constant__ Q8AttendParams p)
 {
-    wait_for_previous_grid();
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float sm_ml[WARPS][Q8_HEADS][2];
     uint4* sm_cs = reinterpret_cast<uint4*>(smem + OFF_CS);
     float4* sm_q = reinterpret_cast<float4*>(smem + OFF_Q);
     float* sm_o = reinterpret_cast<float*>(smem);  // after the loop
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, gq = lane / 4, tq = lane % 4;
+    if (!p.early) wait_for_previous_grid();
+    // cosines and sines of rows 0 .. 63: they do not depend on the grid before this one once the table has been there for a while
+    if (p.table) {
+        for (int i = tid; i < TURN_ROWS * 16; i += THREADS)
+            cp_async16((uint32_t)__cvta_generic_to_shared(sm_cs + i / 16 * CS_ROW + i % 16), p.halves + i, true);
+    } else {
+        for (int i = tid; i < TURN_ROWS * 16; i += THREADS) {
+            const uint32_t x = i % 16 < 8 ? 0x3c003c00u : 0u;  // no RoPE: 1 and 0
+            sm_cs[i / 16 * CS_ROW + i % 16] = make_uint4(x, x, x, x);
+        }
+    }
+    if (p.early) wait_for_previous_grid();
     const int32_t sub = (int32_t)blockIdx.y % p.subs, bh = (int32_t)blockIdx.y / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
     const int32_t len = p.len[b];
     const int32_t rows = p.tiles[b] * TILE, r0 = (int32_t)blockIdx.x * rows, r1 = min(len, r0 + rows);
@@ -206,16 +244,6 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         if (p.table && tile < t1) cp_async16(my_turn + lane * 16, reinterpret_cast<const uint4*>(p.table + (int64_t)(len - 1 - r0 - tile * TILE) * 64) + lane, true);
     };
     fetch(t0, 0);
-    // cosines and sines of rows 0 .. 63
-    if (p.table) {
-        for (int i = tid; i < TURN_ROWS * 16; i += THREADS)
-            cp_async16((uint32_t)__cvta_generic_to_shared(sm_cs + i / 16 * CS_ROW + i % 16), p.halves + i, true);
-    } else {
-        for (int i = tid; i < TURN_ROWS * 16; i += THREADS) {
-            const uint32_t x = i % 16 < 8 ? 0x3c003c00u : 0u;  // no RoPE: 1 and 0
-            sm_cs[i / 16 * CS_ROW + i % 16] = make_uint4(x, x, x, x);
-        }
-    }
     fetch_turn(t0);
     // queries, scaled, before RoPE: lane (gq, tq) reads channels 16 tq + 4 i and 64 + 16 tq + 4 i of head gq at places 4 i + tq, 16 + 4 i + tq
     for (int i = tid; i < Q8_HEADS * 32; i += THREADS) {
@@ -404,9 +432,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     }
     if (!p.tickets || n_splits == 1) return;
     __shared__ int32_t is_last;
-    __threadfence();
     __syncthreads();
     if (tid == 0) {
+        __threadfence();  // of all that the barrier has put before it
         int32_t* t = p.tickets + (bb * p.kv_heads + h) * p.subs + sub;
         const int32_t last = atomicAdd(t, 1) == n_splits - 1;
         if (last) *t = 0;  // for the next launch
@@ -449,7 +477,7 @@ cudaError_t launch(void (*kernel)(const Q8AttendParams), dim3 grid, int smem, co
 int64_t attend_q8_resident(int sm_count) { return (int64_t)sm_count * CTAS_PER_SM; }
 
 cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, const void* q, void* out, int32_t g, const int32_t* lens,
-                             const float2* table, const uint4* halves, float scale, const AttendPlan& plan, float* partial,
+                             const float2* table, const uint4* halves, bool early, float scale, const AttendPlan& plan, float* partial,
                              int32_t* tickets, int32_t* launched, cudaStream_t stream)
 {
     *launched = 0;
@@ -487,6 +515,7 @@ cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, 
     prm.tickets = plan.one_wave && !plan.captured ? tickets : nullptr;
     prm.table = table;
     prm.halves = halves;
+    prm.early = early;
     prm.qscale = scale * 1.4426950408889634f;
     // sequences per launch: their lengths travel as kernel arguments, their groups are rows of the grid
     const int32_t groups = cache.kv_heads * prm.subs, per_launch = std::max(1, std::min(ATTEND_MAX_BATCH, 65535 / groups));

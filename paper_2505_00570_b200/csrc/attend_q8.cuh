@@ -10,10 +10,11 @@ constexpr int Q8_HEADS = 8;  // query heads of one CTA: more heads per KV head a
 inline int32_t q8_head_groups(int32_t q_heads_per_kv) { return (q_heads_per_kv + Q8_HEADS - 1) / Q8_HEADS; }
 // CTAs of the decode kernel that the chip holds at once.
 int64_t attend_q8_resident(int sm_count);
-// q, out: [batch, kv_heads * g, 128] bf16; table: (cos, sin) rows [capacity][64] and its first rows as fp16, or null (no RoPE).  `plan` is one for
+// q, out: [batch, kv_heads * g, 128] bf16; table: (cos, sin) rows [capacity][64] and its first rows as fp16, or null (no RoPE);
+// early: they are known to be finished, whatever is still running.  `plan` is one for
 // kv_heads * q8_head_groups(g) groups a sequence.
 cudaError_t launch_attend_q8(const Q8View& cache, int32_t batch, int32_t layer, const void* q, void* out, int32_t g, const int32_t* lens,
-                             const float2* table, const uint4* halves, float scale, const AttendPlan& plan, float* partial,
+                             const float2* table, const uint4* halves, bool early, float scale, const AttendPlan& plan, float* partial,
                              int32_t* tickets, int32_t* launched, cudaStream_t stream);
 
 }  // namespace freqkv

@@ -45,6 +45,8 @@ struct freqkv_ctx {
     float2* rope_table = nullptr;
     int32_t rope_rows = 0;
     double rope_base = 0.0;
+    cudaEvent_t rope_made = nullptr;  // the table's making; rope_settled: it is known to be over
+    bool rope_settled = false;
     void* attend_work = nullptr;  // attend_ticket_bytes of tickets, then the splits' partials
     size_t attend_work_bytes = 0;
     int32_t* attend_lens = nullptr;  // host: the last call's lengths; what else its split of the rows follows from; that split
