@@ -24,6 +24,7 @@
 
 #include "attend.cuh"
 #include "attend_dev.cuh"
+#include "attend_mass.cuh"
 
 namespace freqkv {
 namespace {
@@ -693,7 +694,8 @@ struct MassParams {
 };
 constexpr int MASS_THREADS = 128, MASS_ROWS = 512;
 
-template <typename T, int G>
+// SCORES: the partial results are attend_scores_kernel's, whose channels lie in another order.
+template <typename T, int G, bool SCORES>
 __global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_constant__ MassParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -726,7 +728,7 @@ __global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_
                 const float* pp = p.partial + (s * heads_total + head0 + g) * PART;
                 acc = fmaf(pp[4 + tid], ex2(pp[0] - sm_m[g]), acc);
             }
-            store1(static_cast<T*>(p.out) + (head0 + g) * 128 + tid, acc * sm_inv[g]);
+            store1(static_cast<T*>(p.out) + (head0 + g) * 128 + (SCORES ? channel_of(tid) : tid), acc * sm_inv[g]);
         }
         return;
     }
@@ -811,11 +813,18 @@ cudaError_t launch_mma(const AttendParams& prm, int32_t g, int32_t nb, int32_t s
 }
 
 template <typename T, int G>
-cudaError_t launch_mass_typed(const AttendParams& prm, const MassParams& fin, int32_t nb, int32_t splits, int32_t longest, bool overlap,
-                              cudaStream_t stream)
+cudaError_t launch_mass_typed(const AttendParams& prm, const MassParams& fin, const freqkv_layout& l, float scale, int32_t nb, int32_t splits,
+                              int32_t longest, bool overlap, cudaStream_t stream)
 {
-    launch_attention(attend_partial_kernel<T, G, false, true>, dim3((unsigned)splits, (unsigned)(nb * prm.kv_heads)), THREADS, 0, stream, prm, overlap);
-    cudaError_t e = cudaGetLastError();
+    constexpr bool SCORES = sizeof(T) == 2 && G >= 2;  // grouped queries of bf16 caches: on the tensor cores
+    cudaError_t e;
+    if constexpr (SCORES) {
+        e = launch_attend_scores(l, prm.k, prm.v, 0, prm.q, G, prm.batch0, nb, prm.len, prm.tiles, splits, prm.table, scale, prm.partial, prm.scores,
+                                 prm.score_rows, overlap, stream);
+    } else {
+        launch_attention(attend_partial_kernel<T, G, false, true>, dim3((unsigned)splits, (unsigned)(nb * prm.kv_heads)), THREADS, 0, stream, prm, overlap);
+        e = cudaGetLastError();
+    }
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((longest + MASS_ROWS - 1) / MASS_ROWS + 1), (unsigned)(nb * prm.kv_heads));
@@ -826,7 +835,7 @@ cudaError_t launch_mass_typed(const AttendParams& prm, const MassParams& fin, in
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, mass_finish_kernel<T, G>, fin);
+    return cudaLaunchKernelEx(&cfg, mass_finish_kernel<T, G, SCORES>, fin);
 }
 
 template <typename T>
@@ -975,6 +984,11 @@ cudaError_t launch_attend(const freqkv_layout& l, const void* k, const void* v, 
     return cudaSuccess;
 }
 
+int64_t attend_mass_resident(int32_t q_heads_per_kv, int32_t dtype, int sm_count)
+{
+    return dtype == FREQKV_BF16 && q_heads_per_kv >= 2 ? attend_scores_resident(sm_count) : attend_resident(q_heads_per_kv, FREQKV_F32, sm_count);
+}
+
 size_t attend_score_bytes(int32_t batch, int32_t q_heads, int32_t capacity)
 {
     return (size_t)batch * q_heads * ((capacity + 31) & ~31) * sizeof(float);
@@ -1028,10 +1042,10 @@ cudaError_t launch_attend_mass(const freqkv_layout& l, const void* k, const void
         auto run = [&](auto t) {
             using T = decltype(t);
             switch (g) {
-                case 1: e = launch_mass_typed<T, 1>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
-                case 2: e = launch_mass_typed<T, 2>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
-                case 4: e = launch_mass_typed<T, 4>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
-                case 8: e = launch_mass_typed<T, 8>(prm, fin, nb, splits, longest, !plan.captured, stream); break;
+                case 1: e = launch_mass_typed<T, 1>(prm, fin, l, scale, nb, splits, longest, !plan.captured, stream); break;
+                case 2: e = launch_mass_typed<T, 2>(prm, fin, l, scale, nb, splits, longest, !plan.captured, stream); break;
+                case 4: e = launch_mass_typed<T, 4>(prm, fin, l, scale, nb, splits, longest, !plan.captured, stream); break;
+                case 8: e = launch_mass_typed<T, 8>(prm, fin, l, scale, nb, splits, longest, !plan.captured, stream); break;
                 default: break;
             }
         };

@@ -34,8 +34,8 @@ cudaError_t launch_attend(const freqkv_layout& l, const void* k, const void* v, 
                           int32_t g, const int32_t* lens_host, const float2* table, float scale, const AttendPlan& plan,
                           float* partial, int32_t* tickets, int32_t* launched, cudaStream_t stream);
 
-// The same with the weights added to mass [batch, layers, kv_heads, capacity]; `scores`: attend_score_bytes.  (CUDA cores: plan for
-// FREQKV_F32's residency.)
+// The same with the weights added to mass [batch, layers, kv_heads, capacity]; `scores`: attend_score_bytes.
+int64_t attend_mass_resident(int32_t q_heads_per_kv, int32_t dtype, int sm_count);
 size_t attend_score_bytes(int32_t batch, int32_t q_heads, int32_t capacity);
 cudaError_t launch_attend_mass(const freqkv_layout& l, const void* k, const void* v, int32_t layer, const void* q, void* out, float* mass,
                                int32_t g, const int32_t* lens_host, const float2* table, float scale, const AttendPlan& plan,

@@ -1,0 +1,378 @@
+// Decode attention that writes its scores down, for bf16 caches with grouped queries: the first of the two kernels behind
+// freqkv_attend_decode_mass there (mass_finish_kernel in attend.cu turns the scores into weights, adds them to the rows' mass
+// and merges the splits' outputs).
+//
+// One pass over the cache rows, 512 bytes of K and V each: bound by memory; at the copy rate an SM has 22 clocks for a row.
+// The sums of weights are kept in fp32, so a score has to be right to a few 2^-22 of its terms -- one fp16 rounding of the turned
+// keys would leave 2^-11.  The CUDA cores are too slow for that with several query heads (8 sequences of 8 x 4 heads, 8 layers: 810 us),
+// so the products run on the matrix instructions with both factors in two fp16 parts, x = hi + lo with 22 bits:
+//   s = k_hi q_hi + k_hi q_lo + k_lo q_hi,
+// three products of m16n8k16 for each 16 channels.  The rest is the arrangement of attend_q8.cu: a warp takes tiles of 16 rows from
+// its own two-stage ring; a lane has 16 consecutive channels and the 16 that RoPE pairs with them of two key rows; keys are turned,
+// in fp32, by their row's place within 64 rows, queries by what is left, once in 64 rows.  Weights enter the second product
+// as two bf16 parts (16 bits), values as they lie in the cache.
+#include <algorithm>
+
+#include "attend_dev.cuh"
+#include "attend_mass.cuh"
+
+namespace freqkv {
+namespace {
+
+constexpr int WARPS = 4, THREADS = 32 * WARPS, CTAS_PER_SM = 2;
+constexpr int TILE = 16, HEADS = 8;
+constexpr int TURN_TILES = 4, TURN_ROWS = TURN_TILES * TILE;
+constexpr int CS_ROW = 36;   // float4 per row of the cosines and sines: 16 + 16, and 4 to spread the rows over the banks
+constexpr int Q_ROW = 36;    // float4 per head likewise
+constexpr int O_ROW = 132;
+constexpr int STAGES = 2, TILE_BYTES = TILE * 256, STAGE_BYTES = 2 * TILE_BYTES;
+constexpr int OFF_CS = WARPS * STAGES * STAGE_BYTES, OFF_TURN = OFF_CS + TURN_ROWS * CS_ROW * 16, OFF_Q = OFF_TURN + WARPS * 512;
+constexpr int SMEM_BYTES = OFF_Q + HEADS * Q_ROW * 16;
+static_assert(WARPS * HEADS * O_ROW * 4 <= OFF_CS, "the merge of the warps reuses the ring");
+static_assert(2 * (SMEM_BYTES + 2048) <= 233472, "two CTAs per SM");
+
+struct ScoreParams {
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;    // moved to the layer
+    int64_t stride_batch, stride_head, stride_token;
+    int32_t kv_heads, g, batch0, total_batch;
+    const __nv_bfloat16* q;
+    float* partial;            // [split][batch][kv_heads * g][PART], channels in the order of channel_of
+    float* scores;
+    int64_t score_rows;
+    const float2* table;
+    float qscale;
+    int32_t len[ATTEND_MAX_BATCH];
+    uint16_t tiles[ATTEND_MAX_BATCH];
+};
+
+// Where the 16-byte chunk ch of row r of a tile lies.  K: lanes (gq, tq) read chunks 2 tq + i and 8 + 2 tq + i of rows gq; V: chunks 2 gq + i
+// of rows 2 tq + const: eight neighbouring lanes in different banks.
+__device__ __forceinline__ uint32_t k_place(int r, int ch) { return (uint32_t)(r * 256 + ((ch ^ (r & 1)) << 4)); }
+__device__ __forceinline__ uint32_t v_place(int r, int ch) { return (uint32_t)(r * 256 + ((ch ^ ((r & 2) >> 1) ^ ((r & 4))) << 4)); }
+
+__device__ __forceinline__ uint4 lds16(const uint8_t* p) { return *reinterpret_cast<const uint4*>(p); }
+__device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+using f2 = unsigned long long;  // two packed fp32
+__device__ __forceinline__ f2 pack(float a, float b)
+{
+    f2 v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ float2 unpack(f2 v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 y;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+    return y;
+}
+// Two fp16 parts of two values.
+__device__ __forceinline__ void split(float2 x, uint32_t& hi, uint32_t& lo)
+{
+    const __half2 h = __floats2half2_rn(x.x, x.y);
+    const float2 f = __half22float2(h);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = pack2_f16(x.x - f.x, x.y - f.y);
+}
+
+__global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(const __grid_constant__ ScoreParams p)
+{
+    wait_for_previous_grid();
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float sm_ml[WARPS][HEADS][2];
+    float4* sm_cs = reinterpret_cast<float4*>(smem + OFF_CS);
+    float4* sm_q = reinterpret_cast<float4*>(smem + OFF_Q);
+    float* sm_o = reinterpret_cast<float*>(smem);  // after the loop
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, gq = lane / 4, tq = lane % 4;
+    const int32_t bh = blockIdx.y, b = bh / p.kv_heads, h = bh % p.kv_heads, heads = p.g;
+    const int32_t len = p.len[b];
+    const int32_t rows = p.tiles[b] * TILE, r0 = (int32_t)blockIdx.x * rows, r1 = min(len, r0 + rows);
+    if (r0 >= len) return;  // a shorter sequence has fewer splits
+    const int32_t n_tiles = (r1 - r0 + TILE - 1) / TILE, per = (n_tiles + WARPS - 1) / WARPS, t0 = min(n_tiles, warp * per), t1 = min(n_tiles, t0 + per);
+    const int64_t bb = p.batch0 + b, head0 = (bb * p.kv_heads + h) * p.g;
+    const __nv_bfloat16* K = p.k + bb * p.stride_batch + h * p.stride_head;
+    const __nv_bfloat16* V = p.v + bb * p.stride_batch + h * p.stride_head;
+
+    const int32_t warp_end = min(r1, r0 + t1 * TILE);
+    uint8_t* ring = smem + warp * (STAGES * STAGE_BYTES);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    // Lane (lane / 16, lane % 16) copies chunk lane % 16 of rows lane / 16 + 2 i; rows past the end become zeros, whose scores are masked.
+    auto fetch = [&](int32_t tile, int stage) {
+        if (tile < t1) {
+            const int32_t j0 = r0 + tile * TILE, row = lane >> 4, ch = lane & 15;
+            const uint32_t at = ring_at + stage * STAGE_BYTES;
+            const bool whole = j0 + TILE <= warp_end;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool there = whole || j0 + row + 2 * i < warp_end;
+                const int64_t off = (int64_t)(there ? j0 + row + 2 * i : j0) * p.stride_token + ch * 8;
+                cp_async16(at + k_place(row + 2 * i, ch), K + off, there);
+                cp_async16(at + TILE_BYTES + v_place(row + 2 * i, ch), V + off, there);
+            }
+        }
+    };
+    // the row of the table that turns the queries for the four tiles from `tile` on
+    const uint32_t my_turn = (uint32_t)__cvta_generic_to_shared(smem) + OFF_TURN + warp * 512;
+    auto fetch_turn = [&](int32_t tile) {
+        if (p.table && tile < t1) cp_async16(my_turn + lane * 16, reinterpret_cast<const uint4*>(p.table + (int64_t)(len - 1 - r0 - tile * TILE) * 64) + lane, true);
+    };
+    fetch(t0, 0);
+    fetch_turn(t0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    // cosines and sines of rows 0 .. 63, four of either together
+    for (int i = tid; i < TURN_ROWS * 16; i += THREADS) {
+        const int r = i / 16, c = i % 16;
+        float4 cs = make_float4(1.f, 1.f, 1.f, 1.f), sn = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p.table) {
+            const float4 a = load(reinterpret_cast<const float4*>(p.table + r * 64 + 4 * c)), d = load(reinterpret_cast<const float4*>(p.table + r * 64 + 4 * c + 2));
+            cs = make_float4(a.x, a.z, d.x, d.z);
+            sn = make_float4(a.y, a.w, d.y, d.w);
+        }
+        const int at = r * CS_ROW + (c & 3) * 4 + c / 4;  // as the queries below
+        sm_cs[at] = cs;
+        sm_cs[at + 16] = sn;
+    }
+    // queries before RoPE: lane (gq, tq) reads channels 16 tq + 4 i and 64 + 16 tq + 4 i of head gq at places 4 i + tq, 16 + 4 i + tq
+    for (int i = tid; i < HEADS * 32; i += THREADS) {
+        const int head = i / 32, c4 = i % 32, half = c4 / 16, quad = c4 % 16;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (head < heads) {
+            const uint2 u = load(reinterpret_cast<const uint2*>(p.q + (head0 + head) * 128 + 4 * c4));
+            x = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+        }
+        sm_q[head * Q_ROW + half * 16 + (quad & 3) * 4 + quad / 4] = x;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+
+    float m_run[2] = {NEG, NEG}, l_run[2] = {0.f, 0.f};
+    float o[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+    uint32_t qh[2][4][2], ql[2][4][2];  // [channels below, from 64][four channels][two pairs]: hi and lo parts
+    const int64_t score0 = (head0 + 2 * tq) * p.score_rows + gq;
+
+    int stage = 0;
+    for (int32_t tile = t0; tile < t1; ++tile, stage ^= 1) {
+        const int32_t j0 = r0 + tile * TILE, sub_tile = (tile - t0) % TURN_TILES;
+        __syncwarp();  // every lane is done with the stage that is filled now
+        fetch(tile + 1, stage ^ 1);
+        if (sub_tile == 0) {
+            const float4* turn = reinterpret_cast<const float4*>(smem + OFF_TURN + warp * 512) + 8 * tq;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                float4 lo = sm_q[gq * Q_ROW + w * 4 + tq], hi = sm_q[gq * Q_ROW + 16 + w * 4 + tq];
+                if (p.table) {
+                    const float4 c0 = turn[2 * w], c1 = turn[2 * w + 1];
+                    rotate(lo.x, hi.x, make_float2(c0.x, c0.y));
+                    rotate(lo.y, hi.y, make_float2(c0.z, c0.w));
+                    rotate(lo.z, hi.z, make_float2(c1.x, c1.y));
+                    rotate(lo.w, hi.w, make_float2(c1.z, c1.w));
+                }
+                split(make_float2(lo.x, lo.y), qh[0][w][0], ql[0][w][0]);
+                split(make_float2(lo.z, lo.w), qh[0][w][1], ql[0][w][1]);
+                split(make_float2(hi.x, hi.y), qh[1][w][0], ql[1][w][0]);
+                split(make_float2(hi.z, hi.w), qh[1][w][1], ql[1][w][1]);
+            }
+            __syncwarp();
+            fetch_turn(tile + TURN_TILES);  // (with the next tile's group: there before it is read, three tiles on)
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        const uint8_t* kt = ring + stage * STAGE_BYTES;
+        const uint8_t* vt = kt + TILE_BYTES;
+
+        // scores of rows gq, gq + 8 and heads 2 tq, 2 tq + 1; small products apart from the large ones
+        float big[2][4], small[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) big[0][i] = big[1][i] = small[0][i] = small[1][i] = 0.f;
+#pragma unroll
+        for (int w2 = 0; w2 < 2; ++w2) {  // eight channels and their partners
+            const uint4 k_lo[2] = {lds16(kt + k_place(gq, 2 * tq + w2)), lds16(kt + k_place(gq + 8, 2 * tq + w2))};
+            const uint4 k_hi[2] = {lds16(kt + k_place(gq, 8 + 2 * tq + w2)), lds16(kt + k_place(gq + 8, 8 + 2 * tq + w2))};
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int w = 2 * w2 + v;
+                uint32_t ah[2][4], al[2][4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float4* cs = sm_cs + (sub_tile * TILE + gq + 8 * r) * CS_ROW + 4 * w + tq;
+                    const float4 c = cs[0], s = cs[16];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t ul = word(k_lo[r], 2 * v + i), uh = word(k_hi[r], 2 * v + i);
+                        const f2 lo = pack(__uint_as_float(ul << 16), __uint_as_float(ul & 0xffff0000u));
+                        const f2 hi = pack(__uint_as_float(uh << 16), __uint_as_float(uh & 0xffff0000u));
+                        const f2 cc = i ? pack(c.z, c.w) : pack(c.x, c.y), ss = i ? pack(s.z, s.w) : pack(s.x, s.y);
+                        const f2 minus = i ? pack(-s.z, -s.w) : pack(-s.x, -s.y);
+                        split(unpack(fma2(hi, minus, mul2(lo, cc))), ah[0][r + 2 * i], al[0][r + 2 * i]);
+                        split(unpack(fma2(lo, ss, mul2(hi, cc))), ah[1][r + 2 * i], al[1][r + 2 * i]);
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    mma_f16(big[x], ah[x], qh[x][w][0], qh[x][w][1]);
+                    mma_f16(small[x], ah[x], ql[x][w][0], ql[x][w][1]);
+                    mma_f16(small[x], al[x], qh[x][w][0], qh[x][w][1]);
+                }
+            }
+        }
+        // running softmax, this thread's rows gq and gq + 8; the scores go out in units of log2
+        float corr[2], pw[2][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = ((small[0][i] + small[1][i]) + (big[0][i] + big[1][i])) * p.qscale;
+        const bool ok0 = j0 + gq < warp_end, ok1 = j0 + gq + 8 < warp_end;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (2 * tq + j < heads) {
+                float* at = p.scores + score0 + j * p.score_rows + j0;
+                if (ok0) at[0] = pw[0][j];
+                if (ok1) at[8] = pw[1][j];
+            }
+        if (!ok0) pw[0][0] = pw[0][1] = -INFINITY;
+        if (!ok1) pw[1][0] = pw[1][1] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float mx = fmaxf(m_run[j], fmaxf(pw[0][j], pw[1][j]));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+            corr[j] = ex2(m_run[j] - mx);
+            m_run[j] = mx;
+            pw[0][j] = ex2(pw[0][j] - mx);
+            pw[1][j] = ex2(pw[1][j] - mx);
+            l_run[j] = fmaf(l_run[j], corr[j], pw[0][j] + pw[1][j]);
+        }
+        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                o[i][0] *= corr[0];
+                o[i][1] *= corr[1];
+                o[i][2] *= corr[0];
+                o[i][3] *= corr[1];
+            }
+        }
+        uint32_t ph[2], pl[2];  // bf16 parts of the weights, as the second product's operand
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const uint32_t hi = pack2_bf16(pw[r][0], pw[r][1]);
+            pl[r] = transpose_8x8(pack2_bf16(pw[r][0] - __uint_as_float(hi << 16), pw[r][1] - __uint_as_float(hi & 0xffff0000u)));
+            ph[r] = transpose_8x8(hi);
+        }
+        // O^T += V^T P: product i takes channels 16 gq + 2 i and + 1
+#pragma unroll
+        for (int w2 = 0; w2 < 2; ++w2) {
+            const uint4 v[4] = {lds16(vt + v_place(2 * tq, 2 * gq + w2)), lds16(vt + v_place(2 * tq + 1, 2 * gq + w2)),
+                                lds16(vt + v_place(2 * tq + 8, 2 * gq + w2)), lds16(vt + v_place(2 * tq + 9, 2 * gq + w2))};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t v0 = word(v[0], i), v1 = word(v[1], i), v2 = word(v[2], i), v3 = word(v[3], i);
+                const uint32_t a[4] = {__byte_perm(v0, v1, 0x5410), __byte_perm(v0, v1, 0x7632), __byte_perm(v2, v3, 0x5410), __byte_perm(v2, v3, 0x7632)};
+                mma_bf16(o[4 * w2 + i], a, pl[0], pl[1]);
+                mma_bf16(o[4 * w2 + i], a, ph[0], ph[1]);
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    __syncthreads();  // the ring makes room
+
+    // merge the warps: channel 16 gq + x at place 8 x + gq, so that a store meets no bank twice
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 4);
+        l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 8);
+        l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 16);
+        const int head = 2 * tq + j;
+        if (gq == 0) {
+            sm_ml[warp][head][0] = m_run[j];
+            sm_ml[warp][head][1] = l_run[j];
+        }
+        float* at = sm_o + (warp * HEADS + head) * O_ROW + gq;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            at[16 * i] = o[i][j];
+            at[16 * i + 8] = o[i][2 + j];
+        }
+    }
+    __syncthreads();
+    for (int32_t g = 0; g < heads; ++g) {
+        float mn = NEG, sum = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) mn = fmaxf(mn, sm_ml[w][g][0]);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = ex2(sm_ml[w][g][0] - mn);
+            sum = fmaf(sm_ml[w][g][1], f, sum);
+            acc = fmaf(sm_o[(w * HEADS + g) * O_ROW + tid], f, acc);
+        }
+        float* part = p.partial + (((int64_t)blockIdx.x * p.total_batch + bb) * p.kv_heads * p.g + h * p.g + g) * PART;
+        part[4 + tid] = acc;
+        if (tid == 0) {
+            part[0] = mn;
+            part[1] = sum;
+        }
+    }
+}
+
+}  // namespace
+
+int64_t attend_scores_resident(int sm_count) { return (int64_t)sm_count * CTAS_PER_SM; }
+
+cudaError_t launch_attend_scores(const freqkv_layout& l, const void* k, const void* v, int32_t layer, const void* q, int32_t g, int32_t batch0,
+                                 int32_t batch_count, const int32_t* lens, const uint16_t* tiles, int32_t splits, const float2* table, float scale,
+                                 float* partial, float* scores, int64_t score_rows, bool overlap, cudaStream_t stream)
+{
+    static PerDeviceOnce attrs;
+    const cudaError_t attr_error = attrs.run([] {
+        cudaError_t e = cudaFuncSetAttribute(attend_scores_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_scores_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        return e;
+    });
+    if (attr_error != cudaSuccess) return attr_error;
+    ScoreParams prm;
+    prm.k = static_cast<const __nv_bfloat16*>(k) + (int64_t)layer * l.stride_layer;
+    prm.v = static_cast<const __nv_bfloat16*>(v) + (int64_t)layer * l.stride_layer;
+    prm.stride_batch = l.stride_batch;
+    prm.stride_head = l.stride_head;
+    prm.stride_token = l.stride_token;
+    prm.kv_heads = l.kv_heads;
+    prm.g = g;
+    prm.batch0 = batch0;
+    prm.total_batch = l.batch;
+    prm.q = static_cast<const __nv_bfloat16*>(q);
+    prm.partial = partial;
+    prm.scores = scores;
+    prm.score_rows = score_rows;
+    prm.table = table;
+    prm.qscale = scale * 1.4426950408889634f;
+    for (int32_t i = 0; i < batch_count; ++i) {
+        prm.len[i] = lens[i];
+        prm.tiles[i] = tiles[i];
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)splits, (unsigned)(batch_count * l.kv_heads));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, attend_scores_kernel, prm);
+}
+
+}  // namespace freqkv

@@ -26,6 +26,7 @@
 #include <algorithm>
 
 #include "attend_dev.cuh"
+#include "attend_mass.cuh"  // channel_of: lanes of equal tq write neighbours, see the merge of the warps
 #include "attend_q8.cuh"
 
 namespace freqkv {
@@ -91,9 +92,6 @@ __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 
 // rows 2 tq + const.  Eight neighbouring lanes then find their chunks in different banks.
 __device__ __forceinline__ uint32_t k_place(int r, int ch) { return (uint32_t)(r * 128 + ((ch ^ ((r & 1) << 2)) << 4)); }
 __device__ __forceinline__ uint32_t v_place(int r, int ch) { return (uint32_t)(r * 128 + ((ch ^ (r & 6)) << 4)); }
-
-// Channel of place t in the partial results: lanes of equal tq write neighbours, see the merge of the warps.
-__device__ __forceinline__ int channel_of(int t) { return (t & 7) * 16 + (t >> 3); }
 
 // All splits of the heads of one CTA's group are there: merge them.  Warps share the heads, and the splits of a head where there
 // are fewer heads than warps.  `sm`: WARPS * (128 + 2) floats.
