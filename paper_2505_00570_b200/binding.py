@@ -573,7 +573,7 @@ class Context:
 
     @staticmethod
     def _per_row(t: torch.Tensor, k: torch.Tensor, dtype: torch.dtype, what: str):
-        if t.dtype != dtype or tuple(t.shape) != tuple(k.shape[:4]) or not t.is_contiguous() or t.device != k.device:
+        if t.dtype != dtype or t.shape != k.shape[:4] or not t.is_contiguous() or t.device != k.device:
             raise FreqKVError(ERR_INVALID_ARG, f"{what} must be dense {dtype} [batch, layers, kv_heads, capacity] on the cache's device")
 
     def attend_decode_mass(self, k: torch.Tensor, v: torch.Tensor, layer: int, q: torch.Tensor, mass: torch.Tensor, lens: list[int],

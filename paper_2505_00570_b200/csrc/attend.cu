@@ -706,15 +706,33 @@ __global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_
     const int32_t j0 = (int32_t)blockIdx.x * MASS_ROWS;
     if (!merges && j0 >= len) return;
     const int64_t heads_total = (int64_t)p.total_batch * p.kv_heads * G, head0 = ((int64_t)(p.batch0 + b) * p.kv_heads + h) * G;
+    float* mass = p.mass + (int64_t)(p.batch0 + b) * p.mass_batch + h * p.mass_rows;
+    // scores and masses travel while the heads' maxima and sums are put together
+    constexpr int PER = MASS_ROWS / MASS_THREADS;
+    float sc[PER][G], had[PER];
+    if (!merges) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int32_t j = min(j0 + i * MASS_THREADS + tid, len - 1);
+#pragma unroll
+            for (int g = 0; g < G; ++g) sc[i][g] = load1(p.scores + (head0 + g) * p.score_rows + j);
+            had[i] = load1(mass + j);
+        }
+    }
     for (int g = warp; g < G; g += MASS_THREADS / 32) {
         const float* base = p.partial + (head0 + g) * PART;
         float mx = NEG, sum = 0.f;
-        for (int s = lane; s < splits; s += 32) mx = fmaxf(mx, base[s * heads_total * PART]);
+        for (int s = lane; s < splits; s += 32) {
+            const float m_s = load1(base + s * heads_total * PART), l_s = load1(base + s * heads_total * PART + 1), m_new = fmaxf(mx, m_s);
+            sum = sum * ex2(mx - m_new) + l_s * ex2(m_s - m_new);
+            mx = m_new;
+        }
 #pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-        for (int s = lane; s < splits; s += 32) sum = fmaf(base[s * heads_total * PART + 1], ex2(base[s * heads_total * PART] - mx), sum);
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        for (int off = 16; off >= 1; off >>= 1) {
+            const float m_o = __shfl_xor_sync(0xffffffffu, mx, off), l_o = __shfl_xor_sync(0xffffffffu, sum, off), m_new = fmaxf(mx, m_o);
+            sum = sum * ex2(mx - m_new) + l_o * ex2(m_o - m_new);
+            mx = m_new;
+        }
         if (lane == 0) {
             sm_m[g] = mx;
             sm_inv[g] = 1.f / sum;
@@ -724,6 +742,7 @@ __global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_
     if (merges) {
         for (int g = 0; g < G; ++g) {
             float acc = 0.f;
+#pragma unroll 4
             for (int s = 0; s < splits; ++s) {
                 const float* pp = p.partial + (s * heads_total + head0 + g) * PART;
                 acc = fmaf(pp[4 + tid], ex2(pp[0] - sm_m[g]), acc);
@@ -732,15 +751,14 @@ __global__ void __launch_bounds__(MASS_THREADS) mass_finish_kernel(const __grid_
         }
         return;
     }
-    float* mass = p.mass + (int64_t)(p.batch0 + b) * p.mass_batch + h * p.mass_rows;
 #pragma unroll
-    for (int i = 0; i < MASS_ROWS / MASS_THREADS; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int32_t j = j0 + i * MASS_THREADS + tid;
         if (j >= len) break;
         float w = 0.f;
 #pragma unroll
-        for (int g = 0; g < G; ++g) w = fmaf(ex2(p.scores[(head0 + g) * p.score_rows + j] - sm_m[g]), sm_inv[g], w);
-        mass[j] += w;
+        for (int g = 0; g < G; ++g) w = fmaf(ex2(sc[i][g] - sm_m[g]), sm_inv[g], w);
+        mass[j] = had[i] + w;
     }
 }
 
