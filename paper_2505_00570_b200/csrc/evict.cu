@@ -19,8 +19,9 @@ namespace freqkv {
 namespace {
 
 constexpr int SELECT_THREADS = 512, SELECT_WARPS = SELECT_THREADS / 32;
+constexpr int ITEMS = 8;  // rows a thread has in hand
 constexpr int BINS = 2048;
-constexpr int MOVE_THREADS = 256, MOVE_UNROLL = 8;
+constexpr int MOVE_THREADS = 256, MOVE_UNROLL = 4;
 
 struct SelectParams {
     const float* mass;
@@ -39,7 +40,7 @@ __device__ __forceinline__ uint32_t ordered(float x)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __grid_constant__ SelectParams p)
+__global__ void __launch_bounds__(SELECT_THREADS, 3) evict_select_kernel(const __grid_constant__ SelectParams p)
 {
     __shared__ uint32_t hist[BINS];
     __shared__ uint2 warp_sum[SELECT_WARPS];
@@ -63,9 +64,15 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
             for (int i = tid; i < BINS; i += SELECT_THREADS) hist[i] = 0;
             __syncthreads();
             const uint32_t mask = (1u << widths[d]) - 1u;
-            for (int32_t j = lo + tid; j < hi; j += SELECT_THREADS) {
-                const uint32_t key = ordered(mass[j]);
-                if (d == 0 || key >> (shifts[d] + widths[d]) == prefix) atomicAdd(&hist[key >> shifts[d] & mask], 1u);
+            for (int32_t j0 = lo + tid; j0 < hi; j0 += SELECT_THREADS * ITEMS) {
+                float m[ITEMS];
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) m[i] = mass[min(j0 + i * SELECT_THREADS, hi - 1)];
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const uint32_t key = ordered(m[i]);
+                    if (j0 + i * SELECT_THREADS < hi && (d == 0 || key >> (shifts[d] + widths[d]) == prefix)) atomicAdd(&hist[key >> shifts[d] & mask], 1u);
+                }
             }
             __syncthreads();
             // thread t has bins BINS - 4 t - 4 .. + 3; how many rows lie above them
@@ -101,26 +108,37 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
         border = prefix;
         equals = want;
     }
-    // places: forced rows and rows above the border count, and the first `equals` rows at it
+    // places: forced rows and rows above the border count, and the first `equals` rows at it.  A warp has 32 * ITEMS neighbouring rows.
     uint32_t base_x = 0, base_y = 0;  // so far: rows that stay whatever the border's equals do; rows at the border
-    for (int32_t j0 = 0; j0 < len; j0 += SELECT_THREADS) {
-        const int32_t j = j0 + tid;
-        float m = 0.f;
-        uint32_t sure = 0, equal = 0;
-        if (j < len) {
-            m = mass[j];
-            if (j < lo || j >= hi) {
-                sure = 1;
-            } else if (heavy > 0) {
-                const uint32_t key = ordered(m);
-                sure = key > border;
-                equal = key == border;
+    for (int32_t j0 = 0; j0 < len; j0 += SELECT_THREADS * ITEMS) {
+        float m[ITEMS];
+        uint32_t sure_bits[ITEMS], equal_bits[ITEMS], x = 0, y = 0;
+        const int32_t first = j0 + warp * (32 * ITEMS) + lane;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) m[i] = first + 32 * i < len ? mass[first + 32 * i] : 0.f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int32_t j = first + 32 * i;
+            bool sure = false, equal = false;
+            if (j < len) {
+                if (j < lo || j >= hi) {
+                    sure = true;
+                } else if (heavy > 0) {
+                    const uint32_t key = ordered(m[i]);
+                    sure = key > border;
+                    equal = key == border;
+                }
             }
+            sure_bits[i] = __ballot_sync(0xffffffffu, sure);
+            equal_bits[i] = __ballot_sync(0xffffffffu, equal);
+            x += __popc(sure_bits[i]);
+            y += __popc(equal_bits[i]);
         }
-        const uint32_t sure_bits = __ballot_sync(0xffffffffu, sure), equal_bits = __ballot_sync(0xffffffffu, equal), below = (1u << lane) - 1u;
-        if (lane == 0) warp_sum[warp] = make_uint2(__popc(sure_bits), __popc(equal_bits));
-        __syncthreads();  // every thread has read its weight, too: mass_out may be mass
-        uint32_t x = base_x + __popc(sure_bits & below), y = base_y + __popc(equal_bits & below);
+        if (lane == 0) warp_sum[warp] = make_uint2(x, y);
+        __syncthreads();  // every thread has read its weights, too: mass_out may be mass
+        x = base_x;
+        y = base_y;
+#pragma unroll
         for (int w = 0; w < SELECT_WARPS; ++w) {
             const uint2 s = warp_sum[w];
             if (w < warp) {
@@ -130,10 +148,16 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const __gr
             base_x += s.x;
             base_y += s.y;
         }
-        if (sure || (equal && y < equals)) {
-            const uint32_t at = x + min(y, equals);
-            rows[at] = j;
-            mass_out[at] = m;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t below = (1u << lane) - 1u, xi = x + __popc(sure_bits[i] & below), yi = y + __popc(equal_bits[i] & below);
+            if ((sure_bits[i] >> lane & 1u) || ((equal_bits[i] >> lane & 1u) && yi < equals)) {
+                const uint32_t at = xi + min(yi, equals);
+                rows[at] = first + 32 * i;
+                mass_out[at] = m[i];
+            }
+            x += __popc(sure_bits[i]);
+            y += __popc(equal_bits[i]);
         }
         __syncthreads();
     }
@@ -164,24 +188,39 @@ __global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const __grid_c
     const bool live = row_in < per_pass && at < row_bytes;
     char* base = static_cast<char*>(tensor_base(p.view, tensor)) +
                  ((int64_t)(p.batch0 + b) * p.view.stride_batch + (int64_t)l * p.view.stride_layer + (int64_t)h * p.view.stride_head) * p.elt + at;
-    // the sinks stay where they are
-    for (int32_t d0 = p.sink; d0 < new_len; d0 += chunk) {
+    struct Rows {
         uint4 v[MOVE_UNROLL];
-        bool moved[MOVE_UNROLL];
+        uint32_t moved;
+    };
+    auto read = [&](Rows& r, int32_t d0) {
+        r.moved = 0;
+        int32_t from[MOVE_UNROLL];
 #pragma unroll
         for (int i = 0; i < MOVE_UNROLL; ++i) {
             const int32_t d = d0 + i * per_pass + row_in;
-            moved[i] = false;
-            if (live && d < new_len) {
-                const int32_t s = rows[d];
-                moved[i] = s != d;
-                if (moved[i]) v[i] = *reinterpret_cast<const uint4*>(base + s * pitch);
-            }
+            from[i] = live && d < new_len ? rows[d] : d;
+            if (from[i] != d) r.moved |= 1u << i;
         }
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < MOVE_UNROLL; ++i)
-            if (moved[i]) *reinterpret_cast<uint4*>(base + (int64_t)(d0 + i * per_pass + row_in) * pitch) = v[i];
+            if (r.moved >> i & 1u) r.v[i] = *reinterpret_cast<const uint4*>(base + from[i] * pitch);
+    };
+    auto write = [&](const Rows& r, int32_t d0) {
+#pragma unroll
+        for (int i = 0; i < MOVE_UNROLL; ++i)
+            if (r.moved >> i & 1u) *reinterpret_cast<uint4*>(base + (int64_t)(d0 + i * per_pass + row_in) * pitch) = r.v[i];
+    };
+    // The sinks stay where they are.  A chunk is written when all of it has been read; the next one, whose rows all lie behind what
+    // is written, is on its way by then.
+    Rows even, odd;
+    read(even, p.sink);
+    for (int32_t d0 = p.sink; d0 < new_len; d0 += 2 * chunk) {
+        __syncthreads();
+        read(odd, d0 + chunk);
+        write(even, d0);
+        __syncthreads();
+        read(even, d0 + 2 * chunk);
+        write(odd, d0 + chunk);
     }
 }
 

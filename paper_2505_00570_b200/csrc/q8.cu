@@ -11,8 +11,9 @@
 //
 // Bound by memory: 2 (or 4) bytes read and 1 written a value.  A block's values stay in registers between the look for their
 // largest magnitude and their rounding, so they are read once: 8 values a chunk, as many chunks a lane as the block's warps (one
-// for every 16 rows) need.  The quotient is taken as a product with 1 / s and looked at again only where it falls within 2^-10
-// of a tie (the product is off by at most 127 * 2^-23): there the remainder, exact in one fma, decides.
+// for every 16 rows) need.  The quotient is taken as a product with 1 / s and looked at again only where it falls within 2^-16
+// of a tie (the product is off by at most 127 * 2^-24): there the remainder, exact in one fma, decides.  It is rounded by adding
+// 1.5 * 2^23, which leaves the code in the sum's low byte.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -98,23 +99,17 @@ __device__ __forceinline__ float scale_of(float largest, int32_t kind)
     return __uint_as_float((uint32_t)max(e, 1) << 23);
 }
 
-// The integer nearest to the quotient x / s, ties to even; inv = 1 / s rounded.  |x| <= 127 s (1 + 2^-22), finite.
-__device__ __forceinline__ float nearest(float x, float s, float inv)
+constexpr float MAGIC = 12582912.f;  // 1.5 * 2^23
+constexpr float NEAR_TIE = 0.5f - 1.f / 65536.f;
+
+// The integer nearest to the quotient x / s, ties to even, where r is the nearest one to x * inv (inv = 1 / s rounded).  |x| <= 127 s (1 + 2^-22).
+__device__ __forceinline__ float decide(float x, float s, float r)
 {
-    const float t = x * inv;
-    float r = rintf(t);
-    if (fabsf(t - r) > 0.4990234375f) {
-        const float rest = fmaf(-r, s, x), off = fabsf(rest) - (s - fabsf(rest));  // both exact: rest is at most s, a multiple of the smaller last place
-        if (off > 0.f || (off == 0.f && ((int)r & 1))) r += rest > 0.f ? 1.f : -1.f;
-    }
+    const float rest = fmaf(-r, s, x), off = fabsf(rest) - (s - fabsf(rest));  // both exact: rest is at most s, a multiple of the smaller last place
+    if (off > 0.f || (off == 0.f && ((int)r & 1))) r += rest > 0.f ? 1.f : -1.f;
     return r;
 }
 
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d)
-{
-    const uint32_t lo = __byte_perm((uint32_t)(int)a, (uint32_t)(int)b, 0x0040), hi = __byte_perm((uint32_t)(int)c, (uint32_t)(int)d, 0x0040);
-    return __byte_perm(lo, hi, 0x5410);
-}
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b)
 {
     return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
@@ -124,13 +119,31 @@ template <int KIND>
 __device__ __forceinline__ uint2 codes_of(float (&x)[8], float s, float inv, bool special)
 {
     if constexpr (KIND == FREQKV_Q8_INT8) {
-        if (special) {
+        if (special) {  // infinities become the largest code, NaN zero
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -127.f * s), 127.f * s) : 0.f;
+            for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? x[i] : 0.f;
         }
+        float sum[8], near_tie = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = fminf(fmaxf(nearest(x[i], s, inv), -127.f), 127.f);
-        return make_uint2(pack4(x[0], x[1], x[2], x[3]), pack4(x[4], x[5], x[6], x[7]));
+        for (int i = 0; i < 8; ++i) {
+            sum[i] = special ? fminf(fmaxf(x[i] * inv, -127.f), 127.f) + MAGIC : fmaf(x[i], inv, MAGIC);
+            near_tie = fmaxf(near_tie, fabsf(fmaf(x[i], inv, MAGIC - sum[i])));
+        }
+        if (near_tie > NEAR_TIE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float r = sum[i] - MAGIC;
+                if (fabsf(x[i]) < INF && fabsf(fmaf(x[i], inv, -r)) > NEAR_TIE) sum[i] = fminf(fmaxf(decide(x[i], s, r), -127.f), 127.f) + MAGIC;
+            }
+        }
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t lo = __byte_perm(__float_as_uint(sum[4 * k]), __float_as_uint(sum[4 * k + 1]), 0x0040);
+            const uint32_t hi = __byte_perm(__float_as_uint(sum[4 * k + 2]), __float_as_uint(sum[4 * k + 3]), 0x0040);
+            w[k] = __byte_perm(lo, hi, 0x5410);
+        }
+        return make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= inv;  // a power of two: exact (what falls below fp32's range rounds to zero in e4m3, too)
@@ -153,7 +166,7 @@ __device__ __forceinline__ uint8_t again(uint8_t code, float s_old, float s)
 
 // A CTA takes 8 / WPB blocks of one matrix, WPB = block_tokens / 16 warps each.  NCH: chunks a lane holds.
 template <typename T, int KIND, int NCH, bool D128>
-__global__ void __launch_bounds__(THREADS) quantize_kernel(const __grid_constant__ WriteParams p)
+__global__ void __launch_bounds__(THREADS, NCH == 8 && sizeof(T) == 2 ? 5 : 1) quantize_kernel(const __grid_constant__ WriteParams p)
 {
     __shared__ float sm_max[WARPS];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
