@@ -34,7 +34,7 @@ struct WriteParams {
     int32_t begin[Q8_MAX_BATCH], end[Q8_MAX_BATCH];
 };
 
-// 8 consecutive values as loaded.
+// 8 consecutive values as loaded, and the largest magnitude of many of them: infinities and NaN show in it.
 template <typename T>
 struct Chunk;
 template <>
@@ -51,13 +51,16 @@ struct Chunk<__nv_bfloat16> {
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
-    // Largest magnitude, NaN if one of the values is NaN.
-    __device__ __forceinline__ float largest() const
+    using Largest = __nv_bfloat162;
+    static __device__ __forceinline__ Largest none() { return __floats2bfloat162_rn(0.f, 0.f); }
+    __device__ __forceinline__ void add_to(Largest& m) const
     {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[0]));
 #pragma unroll
-        for (int i = 1; i < 4; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[i])));
+        for (int i = 0; i < 4; ++i) m = __hmax2_nan(m, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&w[i])));
+    }
+    static __device__ __forceinline__ float value(Largest m)  // NaN if one was
+    {
         const float2 f = __bfloat1622float2(m);
         return f.x != f.x || f.y != f.y ? f.x + f.y : fmaxf(f.x, f.y);
     }
@@ -76,17 +79,16 @@ struct Chunk<float> {
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
         x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     }
-    __device__ __forceinline__ float largest() const
+    using Largest = uint32_t;
+    static __device__ __forceinline__ Largest none() { return 0u; }
+    __device__ __forceinline__ void add_to(Largest& m) const
     {
-        float x[8], m = 0.f, nan = 0.f;
+        float x[8];
         get(x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m = fmaxf(m, fabsf(x[i]));
-            nan += x[i] * 0.f;  // NaN for infinities, too: those blocks take the careful way as well
-        }
-        return nan != nan ? nan : m;
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
     }
+    static __device__ __forceinline__ float value(Largest m) { return __uint_as_float(m); }
 };
 
 __device__ __forceinline__ float scale_of(float largest, int32_t kind)
@@ -115,27 +117,60 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b)
     return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
 
-template <int KIND>
-__device__ __forceinline__ uint2 codes_of(float (&x)[8], float s, float inv, bool special)
+// Two packed fp32 values: half the instructions.
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pack(float a, float b)
 {
+    f2 v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ void unpack(f2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+    return y;
+}
+__device__ __forceinline__ f2 sub2(f2 a, f2 b)
+{
+    f2 y;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+
+// The same 8 values again, one by one: with a tie near, or infinities and NaN among them.
+template <typename T>
+__device__ __noinline__ uint2 careful_int8(const T* p, float s, float inv)
+{
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        const float x = (float)p[i];
+        float r = 0.f;                                           // NaN
+        if (x == x) r = fabsf(x) < INF ? decide(x, s, rintf(x * inv)) : x;
+        w[i / 4] |= ((uint32_t)(int)fminf(fmaxf(r, -127.f), 127.f) & 255u) << 8 * (i % 4);
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+template <int KIND, typename T>
+__device__ __forceinline__ uint2 codes_of(const Chunk<T>& v, const T* from, float s, float inv, bool special)
+{
+    float x[8];
+    v.get(x);
     if constexpr (KIND == FREQKV_Q8_INT8) {
-        if (special) {  // infinities become the largest code, NaN zero
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? x[i] : 0.f;
-        }
         float sum[8], near_tie = 0.f;
+        const f2 inv2 = pack(inv, inv), magic2 = pack(MAGIC, MAGIC);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sum[i] = special ? fminf(fmaxf(x[i] * inv, -127.f), 127.f) + MAGIC : fmaf(x[i], inv, MAGIC);
-            near_tie = fmaxf(near_tie, fabsf(fmaf(x[i], inv, MAGIC - sum[i])));
+        for (int i = 0; i < 4; ++i) {
+            const f2 two = pack(x[2 * i], x[2 * i + 1]), t = fma2(two, inv2, magic2), rest = fma2(two, inv2, sub2(magic2, t));
+            float a, b;
+            unpack(rest, a, b);
+            near_tie = fmaxf(near_tie, fmaxf(fabsf(a), fabsf(b)));
+            unpack(t, sum[2 * i], sum[2 * i + 1]);
         }
-        if (near_tie > NEAR_TIE) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float r = sum[i] - MAGIC;
-                if (fabsf(x[i]) < INF && fabsf(fmaf(x[i], inv, -r)) > NEAR_TIE) sum[i] = fminf(fmaxf(decide(x[i], s, r), -127.f), 127.f) + MAGIC;
-            }
-        }
+        if (special || near_tie > NEAR_TIE) return careful_int8(from, s, inv);
         uint32_t w[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -190,26 +225,38 @@ __global__ void __launch_bounds__(THREADS, NCH == 8 && sizeof(T) == 2 ? 5 : 1) q
 
     const int32_t first = (warp % wpb) * 32 + lane, step = wpb * 32;
     const float s_old = lo < hi && lo > at ? *scale : 0.f;  // rows that are there already
+    // chunk i of this lane: its place in the source and among the codes
+    const bool whole = D128 && hi - lo == bt;
+    const int32_t row0 = first >> 4, c0 = (first & 15) * 8, row_step = step >> 4;  // D128
+    const T* src0 = src + (int64_t)row0 * p.src.stride_token + c0;
+    uint8_t* dst0 = dst + (int64_t)(lo + row0) * p.cache.stride_token + c0;
+    auto from = [&](int i) -> const T* {
+        if constexpr (D128) return src0 + (int64_t)(i * row_step) * p.src.stride_token;
+        const int32_t ch = first + i * step, row = ch / chunks_row;
+        return src + (int64_t)row * p.src.stride_token + (ch - row * chunks_row) * 8;
+    };
+    auto to = [&](int i) -> uint2* {
+        if constexpr (D128) return reinterpret_cast<uint2*>(dst0 + (int64_t)(i * row_step) * p.cache.stride_token);
+        const int32_t ch = first + i * step, row = ch / chunks_row;
+        return reinterpret_cast<uint2*>(dst + (int64_t)(lo + row) * p.cache.stride_token + (ch - row * chunks_row) * 8);
+    };
     Chunk<T> v[NCH];
-    float m = 0.f;
+    typename Chunk<T>::Largest largest = Chunk<T>::none();
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-        const int32_t ch = first + i * step;
-        if (ch < n_chunks) {
-            const int32_t row = D128 ? ch >> 4 : ch / chunks_row, c = (D128 ? ch & 15 : ch - row * chunks_row) * 8;
-            v[i].load(src + (int64_t)row * p.src.stride_token + c);
-        } else {
-            v[i].clear();
-        }
-    }
-    bool special = false;
+        for (int i = 0; i < NCH; ++i) v[i].load(from(i));
+    } else {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-        const float f = v[i].largest();
-        special |= !(f < INF);
-        m = fmaxf(m, f);
+        for (int i = 0; i < NCH; ++i)
+            if (first + i * step < n_chunks)
+                v[i].load(from(i));
+            else
+                v[i].clear();
     }
-    special = __any_sync(0xffffffffu, special);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) v[i].add_to(largest);
+    float m = Chunk<T>::value(largest);
+    const bool special = __any_sync(0xffffffffu, !(m < INF));
     if (special) {  // infinities or NaN among them: the largest finite magnitude, value by value
         m = 0.f;
 #pragma unroll
@@ -231,19 +278,16 @@ __global__ void __launch_bounds__(THREADS, NCH == 8 && sizeof(T) == 2 ? 5 : 1) q
         __syncwarp();
     }
     if (lo >= hi) return;
-    const float s = fmaxf(s_old, scale_of(m, KIND)), inv = s > 0.f ? 1.f / s : 0.f;
+    const float s = fmaxf(s_old, scale_of(m, KIND));
     if (lane == 0 && warp % wpb == 0) *scale = s;
-    const uint2 none = make_uint2(0u, 0u);
+    const float by = s > 0.f ? s : 1.f, inv = 1.f / by;  // (nothing finite but zeros: infinities and NaN still have codes)
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-        const int32_t ch = first + i * step;
-        if (ch < n_chunks) {
-            const int32_t row = D128 ? ch >> 4 : ch / chunks_row, c = (D128 ? ch & 15 : ch - row * chunks_row) * 8;
-            float x[8];
-            v[i].get(x);
-            *reinterpret_cast<uint2*>(dst + (int64_t)(lo + row) * p.cache.stride_token + c) =
-                s > 0.f || special ? codes_of<KIND>(x, s > 0.f ? s : 1.f, s > 0.f ? inv : 1.f, special) : none;
-        }
+        for (int i = 0; i < NCH; ++i) *to(i) = codes_of<KIND>(v[i], from(i), by, inv, special);
+    } else {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+            if (first + i * step < n_chunks) *to(i) = codes_of<KIND>(v[i], from(i), by, inv, special);
     }
     if (lo > at && s > s_old) {  // the scale has grown: the old rows of the block again
         const int32_t old = (lo - at) * chunks_row;
