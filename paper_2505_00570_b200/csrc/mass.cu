@@ -275,8 +275,9 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 64; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], __uint_as_float(sc[j]), __uint_as_float(sc[j + 1]));
                 const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-                const float mc = mx * c;
-                float s4[4] = {total[0] * ex2(fmaf(m, c, -mc)), 0.f, 0.f, 0.f};
+                // (the maximum as multiplied and rounded: where it has not changed the factor is one, not 2^(the product's rounding) for each tile)
+                const float mc = __fmul_rn(mx, c);
+                float s4[4] = {total[0] * ex2(__fmul_rn(m, c) - mc), 0.f, 0.f, 0.f};
                 m = mx;
 #pragma unroll
                 for (int j = 0; j < 64; ++j) s4[j & 3] += ex2(fmaf(__uint_as_float(sc[j]), c, -mc));
@@ -293,7 +294,7 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     *at += (total[0] + total[1]) + (total[2] + total[3]) + o.x;
                 }
             } else {
-                const float mc = fmaxf(m, o.x) * c, l = total[0] * ex2(fmaf(m, c, -mc)) + o.y * ex2(fmaf(o.x, c, -mc));
+                const float mc = __fmul_rn(fmaxf(m, o.x), c), l = total[0] * ex2(__fmul_rn(m, c) - mc) + o.y * ex2(__fmul_rn(o.x, c) - mc);
                 // queries past the chunk's last one: no weight
                 prm.stats[(int64_t)(q_slice0 + q_head) * prm.n_pad + row0 + row] = row0 + row < prm.n_new ? make_float2(mc, 1.f / l) : make_float2(0.f, 0.f);
             }

@@ -239,6 +239,26 @@ def test_chunk_mass_large_against_64_bits_on_the_gpu(ctx):
         assert abs(float(mass[0, 0, h].double().sum()) / (3 * n) - 1) <= 2e-6
 
 
+@pytest.mark.parametrize("n,G", [(2, 1), (3, 4), (5, 1)])
+def test_chunk_mass_of_few_queries_over_many_rows(ctx, n, G):
+    """Running sums over 70 tiles: what each leaves must not add up.  A score's terms are right to 2^-22 and there are fp32 roundings of
+    scores of up to 30 in units of log2 (30 * 2^-24 = 2e-6, ln 2 of it in a weight); sums of 9000 positive terms in 32 chains
+    leave sqrt(280) 2^-24 = 1e-6: 4e-6 in all."""
+    T = 9000
+    k, _ = caches(1, 1, 2, T, torch.bfloat16, 26 + n)
+    q = queries((1, 2 * G, n, 128), torch.bfloat16, 4)
+    mass = torch.zeros(1, 1, 2, T, device="cuda")
+    ctx.attend_mass(k, 0, q, mass, [T])
+    turn = torch.polar(torch.ones((), dtype=torch.float64, device="cuda"),
+                       torch.arange(T, device="cuda").double()[:, None] * 10000.0 ** (-torch.arange(64, device="cuda").double() / 64))
+    z = lambda x, at: torch.complex(x[..., :64].double(), x[..., 64:].double()) * at
+    hidden = torch.full((n, T), -torch.inf, dtype=torch.float64, device="cuda").triu(T - n + 1)
+    for h in range(2):
+        s = (z(q[0, G * h:G * h + G], turn[T - n:]) @ z(k[0, 0, h], turn).conj().T).real / 128 ** 0.5 + hidden
+        want = torch.softmax(s, -1).sum((0, 1))
+        assert float((mass[0, 0, h].double() - want).norm() / want.norm()) <= 4e-6
+
+
 def test_chunk_mass_captured_and_refused(ctx):
     k, _ = caches(1, 2, 2, 300, torch.bfloat16, 25)
     q, mass = queries((1, 4, 70, 128), torch.bfloat16, 4), torch.zeros(1, 2, 2, 300, device="cuda")
