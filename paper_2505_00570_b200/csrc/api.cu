@@ -149,12 +149,12 @@ freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base,
 
 // The layers of a step are attended with the same lengths: the split of their rows (up to 18 candidates x batch divisions, 35 us
 // for a batch of 1000) is worked out once for equal values of everything it follows from.
-AttendPlan attend_plan_for(freqkv_ctx* ctx, int32_t batch, int32_t groups, int64_t resident, const int32_t* lens)
+AttendPlan attend_plan_for(freqkv_ctx* ctx, int32_t batch, int32_t groups, int64_t resident, int32_t overhead_rows, const int32_t* lens)
 {
-    const int32_t key[3] = {batch, groups, (int32_t)resident};
+    const int32_t key[4] = {batch, groups, (int32_t)resident, overhead_rows};
     const size_t bytes = (size_t)batch * sizeof(int32_t);
     if (std::memcmp(key, ctx->attend_key, sizeof(key)) == 0 && std::memcmp(lens, ctx->attend_lens, bytes) == 0) return ctx->attend_last;
-    const AttendPlan plan = attend_plan(batch, lens, groups, resident);
+    const AttendPlan plan = attend_plan(batch, lens, groups, resident, overhead_rows);
     if (batch > ctx->attend_lens_room) {
         std::free(ctx->attend_lens);
         ctx->attend_lens = static_cast<int32_t*>(std::malloc(bytes));
@@ -1166,7 +1166,7 @@ freqkv_status freqkv_attend_decode(freqkv_ctx* ctx, const freqkv_layout* layout,
     const float2* table = nullptr;
     const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
-    AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads, attend_resident(q_heads_per_kv, l.dtype, ctx->sm_count), lens);
+    AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads, attend_resident(q_heads_per_kv, l.dtype, ctx->sm_count), ATTEND_OVERHEAD_ROWS, lens);
     plan.captured = is_capturing(stream);
     AttendWork work;
     const freqkv_status ws = attend_work_for(ctx, plan, l.batch, l.kv_heads * q_heads_per_kv, l.capacity, 0, stream, &work);

@@ -889,14 +889,14 @@ bool attend_supported(int32_t head_dim, int32_t q_heads_per_kv)
 constexpr int32_t MIN_ROWS = 192, MOST_SPLITS = 64;
 
 // Rows of one CTA.  Each candidate is judged by the rows' time of its waves of resident CTAs, waves * (rows +
-// OVERHEAD_ROWS): the constant stands for a CTA's prologue (query, table) and its share of the merge.  A launch with
+// overhead_rows): the constant (ATTEND_OVERHEAD_ROWS here) stands for a CTA's prologue (query, table) and its share of the merge.  A launch with
 // few (sequence, kv head) groups splits down to MIN_ROWS rows, so that even a single sequence is read by the whole
 // chip; one with many groups takes long chunks that fill their last wave.  Measured, us a layer, against two splits
 // of at least 1024 rows: 1 sequence x 8 KV heads x 2611 rows 28.7 -> 13.2 (128 rows 13.4, 256 rows 13.5), 4 x 8 heads of up
-// to 1990 rows 40.7 -> 16.4, 8 x 8 heads of 4099 to 8192 rows 48.9 -> 43.4; OVERHEAD_ROWS 32 and 192 give the same.
-AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int64_t resident)
+// to 1990 rows 40.7 -> 16.4, 8 x 8 heads of 4099 to 8192 rows 48.9 -> 43.4; 32 and 192 overhead rows give the same.
+AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int64_t resident, int32_t overhead_rows)
 {
-    constexpr int32_t OVERHEAD_ROWS = 96, MOST_ROWS = 0xffff * 16;  // a split's tiles are 16 bits
+    constexpr int32_t MOST_ROWS = 0xffff * 16;  // a split's tiles are 16 bits
     const int32_t longest = *std::max_element(lens, lens + batch);
     AttendPlan plan = {};
     int64_t best_cost = -1;
@@ -905,7 +905,7 @@ AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int
         if (splits > 1 && chunk < MIN_ROWS) break;
         int64_t ctas = 0;
         for (int32_t b = 0; b < batch; ++b) ctas += (int64_t)kv_heads * ((lens[b] + chunk - 1) / chunk);
-        const int64_t cost = (ctas + resident - 1) / resident * (chunk + OVERHEAD_ROWS);
+        const int64_t cost = (ctas + resident - 1) / resident * (chunk + overhead_rows);
         if (best_cost < 0 || cost < best_cost) {
             best_cost = cost;
             plan = {chunk, (longest + chunk - 1) / chunk, ctas <= resident};

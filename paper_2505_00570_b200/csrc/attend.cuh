@@ -15,8 +15,9 @@ struct AttendPlan {
     bool one_wave;    // all CTAs are resident at once
     bool captured;    // the launches go into a graph: no tickets, no overlap with the launch before
 };
-// `resident`: CTAs that the chip holds at once.
-AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int64_t resident);
+// `resident`: CTAs that the chip holds at once; `overhead_rows`: what a CTA costs besides its rows, in rows.
+constexpr int32_t ATTEND_OVERHEAD_ROWS = 96;
+AttendPlan attend_plan(int32_t batch, const int32_t* lens, int32_t kv_heads, int64_t resident, int32_t overhead_rows);
 int64_t attend_resident(int32_t q_heads_per_kv, int32_t dtype, int sm_count);
 // No plan for lengths up to `longest` has more splits (unless rows beyond what 64 CTAs can take force them).
 int32_t attend_most_splits(int32_t longest);

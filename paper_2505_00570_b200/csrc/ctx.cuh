@@ -50,7 +50,7 @@ struct freqkv_ctx {
     void* attend_work = nullptr;  // attend_ticket_bytes of tickets, then the splits' partials
     size_t attend_work_bytes = 0;
     int32_t* attend_lens = nullptr;  // host: the last call's lengths; what else its split of the rows follows from; that split
-    int32_t attend_lens_room = 0, attend_key[3] = {0, 0, 0};
+    int32_t attend_lens_room = 0, attend_key[4] = {0, 0, 0, 0};
     freqkv::AttendPlan attend_last = {};
     bool attend_tickets_clear = false;  // zeroed on a stream that later calls are ordered behind
     void* prefill_keys = nullptr;     // rotated keys of one layer, fp16
@@ -107,7 +107,7 @@ freqkv_status rope_table_for(freqkv_ctx* ctx, int32_t capacity, float rope_base,
 
 // The split of the rows of a decode attention of `groups` (kv head, ...) groups a sequence; the work area of the call: tickets, the
 // splits' partials of q_heads heads a sequence, `more` bytes for the caller (256-byte aligned).
-AttendPlan attend_plan_for(freqkv_ctx* ctx, int32_t batch, int32_t groups, int64_t resident, const int32_t* lens);
+AttendPlan attend_plan_for(freqkv_ctx* ctx, int32_t batch, int32_t groups, int64_t resident, int32_t overhead_rows, const int32_t* lens);
 struct AttendWork {
     int32_t* tickets;
     float* partial;
