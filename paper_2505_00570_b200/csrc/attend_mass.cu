@@ -230,8 +230,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
                 }
             }
         }
-        // running softmax, this thread's rows gq and gq + 8; the scores go out in units of log2
-        float corr[2], pw[2][2];
+        // this thread's rows gq and gq + 8; the scores go out in units of log2
+        float pw[2][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = ((small[0][i] + small[1][i]) + (big[0][i] + big[1][i])) * p.qscale;
         const bool ok0 = j0 + gq < warp_end, ok1 = j0 + gq + 8 < warp_end;
@@ -244,19 +244,22 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
             }
         if (!ok0) pw[0][0] = pw[0][1] = -INFINITY;
         if (!ok1) pw[1][0] = pw[1][1] = -INFINITY;
+        // softmax against a reference that moves (to the maximum so far) only when a score is more than 2^8 above it
+        float most[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float mx = fmaxf(m_run[j], fmaxf(pw[0][j], pw[1][j]));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            corr[j] = ex2(m_run[j] - mx);
-            m_run[j] = mx;
-            pw[0][j] = ex2(pw[0][j] - mx);
-            pw[1][j] = ex2(pw[1][j] - mx);
-            l_run[j] = fmaf(l_run[j], corr[j], pw[0][j] + pw[1][j]);
-        }
-        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+        for (int j = 0; j < 2; ++j) most[j] = fmaxf(pw[0][j], pw[1][j]);
+        if (__any_sync(0xffffffffu, fmaxf(most[0] - m_run[0], most[1] - m_run[1]) > 8.f)) {
+            float corr[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float mx = most[j];
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                mx = fmaxf(fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16)), m_run[j]);
+                corr[j] = ex2(m_run[j] - mx);
+                m_run[j] = mx;
+                l_run[j] *= corr[j];
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 o[i][0] *= corr[0];
@@ -265,6 +268,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
                 o[i][3] *= corr[1];
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = ex2(pw[i / 2][i % 2] - m_run[i % 2]);
+        l_run[0] += pw[0][0] + pw[1][0];
+        l_run[1] += pw[0][1] + pw[1][1];
         uint32_t ph[2], pl[2];  // bf16 parts of the weights, as the second product's operand
 #pragma unroll
         for (int r = 0; r < 2; ++r) {

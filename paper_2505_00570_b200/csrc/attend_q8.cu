@@ -35,6 +35,7 @@ namespace {
 constexpr int WARPS = 8, THREADS = 32 * WARPS, CTAS_PER_SM = 2;
 static_assert(CTAS_PER_SM <= ATTEND_MOST_CTAS_PER_SM, "tickets");
 constexpr int TILE = 16;
+constexpr float REFERENCE_STEP = 8.f;         // log2 of the largest weight
 constexpr int TURN_TILES = 4;                 // tiles whose queries are turned alike
 constexpr int TURN_ROWS = TURN_TILES * TILE;
 constexpr int CS_ROW = 17;   // uint4 per row of the cosines and sines: 8 + 8, and one to spread the rows over the banks
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
 
-    float m_run[2] = {NEG, NEG}, l_run[2] = {0.f, 0.f}, vref = 0.f, vinv = 0.f;
+    float m_ref[2] = {NEG, NEG}, l_run[2] = {0.f, 0.f}, vref = 0.f, vinv = 0.f;
     float o[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -326,35 +327,38 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
                 }
             }
         }
-        // running softmax, this thread's rows gq and gq + 8
-        float corr[2], pw[2][2];
+        // softmax, this thread's rows gq and gq + 8, against a reference that moves (to the maximum so far) only when a score is more
+        // than 2^8 above it: the maximum over the lanes, and the factors for what has been summed, are rarely needed
+        float pw[2][2];
+        auto against = [&] {  // the scores less the reference; rows past the end have none
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = (s0[i] + s1[i]) * ks;
-        if (j0 + TILE > warp_end) {
-            if (j0 + gq >= warp_end) pw[0][0] = pw[0][1] = -INFINITY;
-            if (j0 + gq + 8 >= warp_end) pw[1][0] = pw[1][1] = -INFINITY;
-        }
+            for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = fmaf(s0[i] + s1[i], ks, -m_ref[i % 2]);
+            if (j0 + TILE > warp_end) {
+                if (j0 + gq >= warp_end) pw[0][0] = pw[0][1] = -INFINITY;
+                if (j0 + gq + 8 >= warp_end) pw[1][0] = pw[1][1] = -INFINITY;
+            }
+        };
+        against();
+        if (__any_sync(0xffffffffu, fmaxf(fmaxf(pw[0][0], pw[0][1]), fmaxf(pw[1][0], pw[1][1])) > REFERENCE_STEP || vs > vref)) {
+            float corr[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float mx = fmaxf(m_run[j], fmaxf(pw[0][j], pw[1][j]));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-            corr[j] = ex2(m_run[j] - mx);
-            m_run[j] = mx;
-            pw[0][j] = ex2(pw[0][j] - mx);
-            pw[1][j] = ex2(pw[1][j] - mx);
-            l_run[j] = fmaf(l_run[j], corr[j], pw[0][j] + pw[1][j]);
-        }
-        if (vs > vref) {  // the weights' unit grows
-            const float f = vref / vs;
-            corr[0] *= f;
-            corr[1] *= f;
-            vref = vs;
-            vinv = 1.f / vref;
-        }
-        const float unit = vs * vinv;
-        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+            for (int j = 0; j < 2; ++j) {
+                float mx = fmaxf(j0 + gq < warp_end ? (s0[j] + s1[j]) * ks : NEG, j0 + gq + 8 < warp_end ? (s0[2 + j] + s1[2 + j]) * ks : NEG);
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                mx = fmaxf(fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16)), m_ref[j]);
+                corr[j] = ex2(m_ref[j] - mx);
+                m_ref[j] = mx;
+                l_run[j] *= corr[j];
+            }
+            against();
+            if (vs > vref) {  // the weights' unit grows
+                const float f = vref / vs;
+                corr[0] *= f;
+                corr[1] *= f;
+                vref = vs;
+                vinv = 1.f / vref;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 o[i][0] *= corr[0];
@@ -363,6 +367,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
                 o[i][3] *= corr[1];
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = ex2(pw[i / 2][i % 2]);
+        l_run[0] += pw[0][0] + pw[1][0];
+        l_run[1] += pw[0][1] + pw[1][1];
+        const float unit = vs * vinv;
         const uint32_t p0 = transpose_8x8(pack2_f16(pw[0][0] * unit, pw[0][1] * unit));
         const uint32_t p1 = transpose_8x8(pack2_f16(pw[1][0] * unit, pw[1][1] * unit));
         // O^T += V^T P: product i takes channels 16 gq + 2 i and + 1
@@ -394,7 +403,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 16);
         const int head = 2 * tq + j;
         if (gq == 0) {
-            sm_ml[warp][head][0] = m_run[j];
+            sm_ml[warp][head][0] = m_ref[j];
             sm_ml[warp][head][1] = l_run[j];
         }
         float* at = sm_o + (warp * Q8_HEADS + head) * O_ROW + gq;
