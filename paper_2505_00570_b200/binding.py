@@ -504,11 +504,12 @@ class Context:
         lay = cache.layout
         if not (new_k.is_contiguous() and new_v.is_contiguous()) or new_k.shape != new_v.shape or new_k.dtype != new_v.dtype:
             raise FreqKVError(ERR_INVALID_ARG, "new_k / new_v must be dense and of equal shape and dtype")
-        if new_k.dim() != 5 or new_k.shape[:3] != cache.k.shape[:3] or new_k.shape[4] != cache.k.shape[4] or len(lens) != lay.batch:
+        shape = new_k.shape
+        if len(shape) != 5 or (shape[0], shape[1], shape[2], shape[4]) != (lay.batch, lay.layers, lay.kv_heads, lay.head_dim) or len(lens) != lay.batch:
             raise FreqKVError(ERR_INVALID_ARG, "new rows or lens do not match the cache")
         c_lens = (c_int32 * lay.batch)(*lens)
         st = lib().freqkv_append_q8(self._h, cache._ref, *cache._ptrs, new_k.data_ptr(), new_v.data_ptr(), dtype_code(new_k.dtype),
-                                    new_k.shape[3], c_lens, _stream_ptr(stream))
+                                    shape[3], c_lens, _stream_ptr(stream))
         self._check(st, "freqkv_append_q8")
         return list(c_lens)
 

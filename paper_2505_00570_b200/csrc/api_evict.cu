@@ -43,7 +43,7 @@ freqkv_status freqkv_attend_decode_mass(freqkv_ctx* ctx, const freqkv_layout* la
     const freqkv_status ts = rope_table_for(ctx, std::max(l.capacity, ROPE_HALF_ROWS), rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
     AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads, attend_mass_resident(q_heads_per_kv, l.dtype, ctx->sm_count), ATTEND_OVERHEAD_ROWS, lens);
-    plan.captured = is_capturing(stream);
+    plan.captured = order.captured;
     plan.one_wave = false;  // no tickets: a second kernel follows anyway
     AttendWork work;
     const int32_t heads = l.kv_heads * q_heads_per_kv;

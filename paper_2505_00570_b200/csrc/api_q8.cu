@@ -229,7 +229,7 @@ freqkv_status freqkv_attend_decode_q8(freqkv_ctx* ctx, const freqkv_q8_layout* l
     const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
     AttendPlan plan = attend_plan_for(ctx, l.batch, l.kv_heads * q8_head_groups(q_heads_per_kv), attend_q8_resident(ctx->sm_count), Q8_OVERHEAD_ROWS, lens);
-    plan.captured = is_capturing(stream);
+    plan.captured = order.captured;
     AttendWork work;
     const freqkv_status ws = attend_work_for(ctx, plan, l.batch, l.kv_heads * q_heads_per_kv, l.capacity, 0, stream, &work);
     if (ws != FREQKV_OK) return ws;

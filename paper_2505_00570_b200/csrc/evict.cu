@@ -58,6 +58,8 @@ __global__ void __launch_bounds__(SELECT_THREADS, 3) evict_select_kernel(const _
     uint32_t border = 0xffffffffu, equals = 0;
     if (heavy > 0) {
         uint32_t prefix = 0, want = (uint32_t)heavy;  // of the rows that share the digits so far
+        const bool once = hi - lo <= SELECT_THREADS * ITEMS;  // then the weights stay in registers from digit to digit
+        uint32_t key[ITEMS];
         const int shifts[3] = {21, 10, 0}, widths[3] = {11, 11, 10};
 #pragma unroll
         for (int d = 0; d < 3; ++d) {
@@ -65,14 +67,17 @@ __global__ void __launch_bounds__(SELECT_THREADS, 3) evict_select_kernel(const _
             __syncthreads();
             const uint32_t mask = (1u << widths[d]) - 1u;
             for (int32_t j0 = lo + tid; j0 < hi; j0 += SELECT_THREADS * ITEMS) {
-                float m[ITEMS];
+                if (d == 0 || !once) {
+                    float m[ITEMS];
 #pragma unroll
-                for (int i = 0; i < ITEMS; ++i) m[i] = mass[min(j0 + i * SELECT_THREADS, hi - 1)];
+                    for (int i = 0; i < ITEMS; ++i) m[i] = mass[min(j0 + i * SELECT_THREADS, hi - 1)];
 #pragma unroll
-                for (int i = 0; i < ITEMS; ++i) {
-                    const uint32_t key = ordered(m[i]);
-                    if (j0 + i * SELECT_THREADS < hi && (d == 0 || key >> (shifts[d] + widths[d]) == prefix)) atomicAdd(&hist[key >> shifts[d] & mask], 1u);
+                    for (int i = 0; i < ITEMS; ++i) key[i] = ordered(m[i]);
                 }
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i)
+                    if (j0 + i * SELECT_THREADS < hi && (d == 0 || key[i] >> (shifts[d] + widths[d]) == prefix))
+                        atomicAdd(&hist[key[i] >> shifts[d] & mask], 1u);
             }
             __syncthreads();
             // thread t has bins BINS - 4 t - 4 .. + 3; how many rows lie above them
@@ -174,6 +179,7 @@ struct MoveParams {
 
 __global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const __grid_constant__ MoveParams p)
 {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched with programmatic stream serialization, behind the kernel that selects
     const int32_t slice = (int32_t)(blockIdx.x % (uint32_t)p.slices);
     const int64_t mat = blockIdx.x / (uint32_t)p.slices;
     const int tensor = (int)(mat & 1);
@@ -265,8 +271,16 @@ cudaError_t launch_evict(const CacheView& view, int32_t dtype, int32_t batch, in
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         ++*launched;
-        evict_move_kernel<<<(unsigned)(2 * triples * mov.slices), MOVE_THREADS, 0, stream>>>(mov);
-        e = cudaGetLastError();
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(2 * triples * mov.slices));
+        cfg.blockDim = dim3(MOVE_THREADS);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, evict_move_kernel, mov);
         if (e != cudaSuccess) return e;
         ++*launched;
     }
