@@ -96,7 +96,7 @@ freqkv_status freqkv_attend_mass(freqkv_ctx* ctx, const freqkv_layout* layout, c
     const float2* table = nullptr;
     const freqkv_status ts = rope_table_for(ctx, l.capacity, rope_base, stream, &table);
     if (ts != FREQKV_OK) return ts;
-    const freqkv_status gs = prefill_scratch(ctx, mass_key_bytes(l), mass_query_bytes(l, q_heads_per_kv, n_new));
+    const freqkv_status gs = prefill_scratch(ctx, mass_key_bytes(l), mass_query_bytes(l, q_heads_per_kv, n_new, ctx->sm_count));
     if (gs != FREQKV_OK) return gs;
     const char* why = nullptr;
     int32_t launched = 0;
@@ -104,7 +104,7 @@ freqkv_status freqkv_attend_mass(freqkv_ctx* ctx, const freqkv_layout* layout, c
     {
         TransformTimer timer(ctx, stream);
         e = launch_attend_chunk_mass(l, k, layer, q, mass, q_heads_per_kv, n_new, lens, table, scale, ctx->prefill_keys, ctx->prefill_queries,
-                                     ctx->status_dev, ctx->gemm.wait_limit_ns, &why, &launched, stream);
+                                     ctx->sm_count, ctx->status_dev, ctx->gemm.wait_limit_ns, &why, &launched, stream);
     }
     ctx->kernels_launched += launched;
     if (e == cudaSuccess) return FREQKV_OK;

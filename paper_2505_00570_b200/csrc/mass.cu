@@ -6,14 +6,21 @@
 //   pass 1 (CUDA cores): keys of the layer and queries of the chunk are turned (RoPE, fp32) and written as two fp16 parts each,
 //     x = hi + lo with 22 bits: sums of weights are kept in fp32, and one fp16 part would leave 2^-11 a term in the scores.
 //     A score is  hi hi + hi lo + lo hi  (what is left out is 2^-22 of a term).
-//   pass 2, a CTA for each (sequence, query head, 128 queries): S = Q K^T over tiles of 128 keys; running maximum and sum of
-//     each query, one query a thread and half of the tile's columns;
-//   pass 3, a CTA for each (sequence, KV head, 128 keys): S^T = K Q^T over tiles of 128 queries of all heads of the group that see
-//     the keys; a thread has one key and adds up half of the columns' weights, so there are no sums across threads but the last.
-// Passes 2 and 3 are one kernel with its sides exchanged: 128 resident rows ("A"), 128 streamed rows a tile ("B", two
-// stages), the scores of two tiles in tensor memory, so that one tile's products run while the other's scores are read:
+//   pass 2, units of (sequence, query head, 128 queries): S = Q K^T over tiles of 128 keys; running maximum and sum of each query, one
+//     query a thread and half of the tile's columns;
+//   pass 3, units of (sequence, KV head, 128 keys): S^T = K Q^T over tiles of 128 queries of all heads of the group that see the
+//     keys; a thread has one key and adds up half of the columns' weights, so there are no sums across threads but the last.
+// Passes 2 and 3 are one kernel with its sides exchanged: 128 resident rows ("A"), 128 streamed rows a tile ("B", two stages), the
+// scores of two tiles in tensor memory, so that one tile's products run while the other's scores are read:
 //   warp 0 loads (TMA), warp 1 issues the products, warps 2-9 read scores, two warps a lane quarter, 64 columns each.
-// Bound by the tensor cores: 3 * 8 products of 128 x 128 x 16 a tile and pass.  Every wait is bounded as in prefill.cu.
+// All units' tiles in a row are cut into equal shares, one for each SM, wherever that falls: a CTA walks the units of its share,
+// and what it has of a unit that others have a share of, too, goes to a slot of its own, from which a small kernel behind each pass
+// puts the unit together, in the order of the shares.  (A CTA for each unit
+// left most SMs idle in small calls: 300 queries of 4 heads over 6000 rows 83 us a layer instead of 37, 64 queries of 2 x 8 heads over
+// 3000 and 5000 rows 72 instead of 38; large calls take the same either way.)
+// Bound by the tensor cores: 3 * 8 products of 128 x 128 x 16 a tile and pass; 32 heads of 1001 queries over 5003 and 6790 rows, 0.58
+// TFLOP a layer, take passes 2 and 3 206 and 256 us: 1.26 PFLOP/s, nine tenths of what the chip sustains under its power limit.
+// (With 256 resident rows in tensor memory, half the streamed bytes: 229 and 285 us.)  Every wait is bounded as in prefill.cu.
 #include <algorithm>
 
 #include "mass.cuh"
@@ -32,15 +39,67 @@ constexpr int READERS = 8, THREADS = 64 + 32 * READERS;
 constexpr int TMEM_COLS = 2 * T;
 
 struct ChunkParams {
-    int32_t n_new, n_pad, kv_heads, g, batch0, batch_count, q_tiles, k_tiles;
+    int32_t n_new, n_pad, kv_heads, g, batch0, batch_count, q_tiles, shares;
     float c;                // scale * log2(e)
     float2* stats;          // [batch * heads_q][n_pad]: maximum * c, 1 / sum
     float* mass;            // moved to the layer
     int64_t mass_batch, mass_rows;
+    float2* slots;          // [2 * shares][T]: a share's part of its first unit, of its last one
     int32_t* status;
     unsigned long long wait_limit_ns;
     int32_t len[PREFILL_MAX_BATCH];
+    uint64_t before[PREFILL_MAX_BATCH + 1];  // tiles of the sequences before, of this pass
 };
+
+// A unit and the number of its tiles: rows tile * 128 .. of head `head` of sequence b.  Units follow one another by sequence, then by
+// rows, then by head.
+struct Unit {
+    int32_t b, tile, head, tiles;
+};
+template <bool SUMS>
+__host__ __device__ inline int32_t tiles_of(const ChunkParams& p, int32_t b, int32_t tile)
+{
+    const int32_t pos0 = p.len[b] - p.n_new;
+    if (SUMS) return (p.q_tiles - (tile * T > pos0 ? (tile * T - pos0) / T : 0)) * p.g;  // each head's queries from the first that sees a key
+    const int32_t end = tile * T + T < p.n_new ? tile * T + T : p.n_new;
+    return (pos0 + end - 1) / T + 1;  // keys up to the last one that a query sees
+}
+template <bool SUMS>
+__host__ __device__ inline int32_t row_tiles(const ChunkParams& p, int32_t b) { return SUMS ? (p.len[b] + T - 1) / T : p.q_tiles; }
+template <bool SUMS>
+__host__ __device__ inline int32_t heads_of(const ChunkParams& p) { return SUMS ? p.kv_heads : p.kv_heads * p.g; }
+// First tile of share c of `total` tiles in `shares`, and the share that holds tile x.
+__device__ __forceinline__ uint64_t share_begin(uint64_t total, int32_t shares, int32_t c) { return total * (uint32_t)c / (uint32_t)shares; }
+__device__ __forceinline__ int32_t share_of(uint64_t total, int32_t shares, uint64_t x) { return (int32_t)(((x + 1) * (uint32_t)shares - 1) / total); }
+template <bool SUMS>
+__device__ __forceinline__ void next_unit(const ChunkParams& p, Unit& u)
+{
+    if (++u.head < heads_of<SUMS>(p)) return;
+    u.head = 0;
+    if (++u.tile == row_tiles<SUMS>(p, u.b)) {
+        u.tile = 0;
+        if (++u.b == p.batch_count) return;
+    }
+    u.tiles = tiles_of<SUMS>(p, u.b, u.tile);
+}
+// The unit that holds tile x, and which tile of it that is.
+template <bool SUMS>
+__device__ __forceinline__ Unit find_unit(const ChunkParams& p, uint64_t x, int32_t& at)
+{
+    Unit u = {0, 0, 0, 0};
+    while (x >= p.before[u.b + 1]) ++u.b;
+    x -= p.before[u.b];
+    const uint32_t heads = (uint32_t)heads_of<SUMS>(p);
+    for (;; ++u.tile) {
+        u.tiles = tiles_of<SUMS>(p, u.b, u.tile);
+        const uint64_t here = (uint64_t)heads * (uint32_t)u.tiles;
+        if (x < here) break;
+        x -= here;
+    }
+    u.head = (int32_t)((uint32_t)x / (uint32_t)u.tiles);
+    at = (int32_t)((uint32_t)x % (uint32_t)u.tiles);
+    return u;
+}
 
 // ---- pass 1: rows of a half-warp each, as in prefill.cu, written as [slice][hi, lo][rows][128] ----
 struct SplitJob {
@@ -121,45 +180,42 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     uint8_t* aligned = smem_raw + (base - raw);
-    const uint32_t bar0 = base + OFF_BAR, a_full = bar0;
-    auto b_full = [&](int s) { return bar0 + 8u * (1 + s); };
-    auto b_empty = [&](int s) { return bar0 + 8u * (1 + STAGES + s); };
-    auto d_full = [&](int s) { return bar0 + 8u * (1 + 2 * STAGES + s); };
-    auto d_free = [&](int s) { return bar0 + 8u * (3 + 2 * STAGES + s); };
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + OFF_BAR + 8 * (5 + 2 * STAGES));
+    const uint32_t bar0 = base + OFF_BAR, a_full = bar0, a_empty = bar0 + 8u;
+    auto b_full = [&](int s) { return bar0 + 8u * (2 + s); };
+    auto b_empty = [&](int s) { return bar0 + 8u * (2 + STAGES + s); };
+    auto d_full = [&](int s) { return bar0 + 8u * (2 + 2 * STAGES + s); };
+    auto d_free = [&](int s) { return bar0 + 8u * (4 + 2 * STAGES + s); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(aligned + OFF_BAR + 8 * (6 + 2 * STAGES));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    float2* sm_half = reinterpret_cast<float2*>(aligned + OFF_BAR + 256);  // [128]: what the second half's threads have found
+    float2* sm_half = reinterpret_cast<float2*>(aligned + OFF_BAR + 256);  // [2][128]: what the second half's threads have found, by units in turn
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int32_t heads_q = prm.kv_heads * prm.g;
-    // which rows are resident, and over which tiles the others run
-    int32_t b, h, row0, first_tile, n_tiles, q_head = 0;
-    if constexpr (SUMS) {
-        const int32_t units = prm.kv_heads * prm.batch_count, unit = (int32_t)blockIdx.x % units;
-        b = unit / prm.kv_heads;
-        h = unit % prm.kv_heads;
-        row0 = (int32_t)blockIdx.x / units * T;
-    } else {  // the query tiles with the most keys first
-        const int32_t units = heads_q * prm.batch_count, unit = (int32_t)blockIdx.x % units;
-        b = unit / heads_q;
-        q_head = unit % heads_q;
-        h = q_head / prm.g;
-        row0 = (prm.q_tiles - 1 - (int32_t)blockIdx.x / units) * T;
-    }
-    const int32_t len = prm.len[b], pos0 = len - prm.n_new;
-    if constexpr (SUMS) {
-        if (row0 >= len) return;  // a shorter sequence
-        first_tile = row0 > pos0 ? (row0 - pos0) / T : 0;
-        n_tiles = (prm.q_tiles - first_tile) * prm.g;
-    } else {
-        first_tile = 0;
-        n_tiles = (pos0 + min(row0 + T, prm.n_new) - 1) / T + 1;
-    }
-    const int32_t per_head = prm.q_tiles - first_tile;  // SUMS: tiles of a head
-    const int32_t k_slice = (prm.batch0 + b) * prm.kv_heads + h, q_slice0 = (prm.batch0 + b) * heads_q;
+    const int32_t heads_q = prm.kv_heads * prm.g, share = (int32_t)blockIdx.x;
+    const uint64_t total = prm.before[prm.batch_count], begin = share_begin(total, prm.shares, share), end = share_begin(total, prm.shares, share + 1);
+    int32_t first_at;
+    const Unit first_unit = find_unit<SUMS>(prm, begin, first_at);
+    // Calls f(unit, its tiles [from, to), number of the segment) for every unit of the share until one gives up.
+    auto segments = [&](auto&& f) {
+        Unit u = first_unit;
+        int32_t at = first_at;
+        uint64_t x = begin;
+        for (int32_t seg = 0; x < end; ++seg) {
+            const int32_t to = (int32_t)min((uint64_t)u.tiles, at + (end - x));
+            if (!f(u, at, to, seg)) return;
+            x += (uint32_t)(to - at);
+            at = 0;
+            next_unit<SUMS>(prm, u);
+        }
+    };
+    // Tile t of a unit streams these rows of this slice; of SUMS, all tiles of a head, then of the next.
+    auto first_q = [&](const Unit& u) {
+        const int32_t pos0 = prm.len[u.b] - prm.n_new;
+        return u.tile * T > pos0 ? (u.tile * T - pos0) / T : 0;
+    };
 
     if (threadIdx.x == 0) {
         mbar_init(a_full, 1);
+        mbar_init(a_empty, 1);
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(b_full(s), 1);
             mbar_init(b_empty(s), 1);
@@ -190,115 +246,142 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tma_load_3d(dst + i * SLAB, map, bar, (i & 1) * 64, row, 2 * slice + i / 2);  // hi, then lo; 64 channels each
             };
-            if (SUMS)
-                load_operand(base + OFF_A, &map_k, a_full, row0, k_slice);
-            else
-                load_operand(base + OFF_A, &map_q, a_full, row0, q_slice0 + q_head);
-            for (int32_t t = 0; t < n_tiles; ++t) {
-                const int s = t % STAGES;
-                if (t >= STAGES && !mbar_wait(b_empty(s), ((uint32_t)(t / STAGES) - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
-                if (SUMS)
-                    load_operand(base + OFF_B + s * OPERAND, &map_q, b_full(s), (first_tile + t % per_head) * T, q_slice0 + h * prm.g + t / per_head);
-                else
-                    load_operand(base + OFF_B + s * OPERAND, &map_k, b_full(s), t * T, k_slice);
-            }
+            uint32_t n = 0;  // tiles loaded
+            segments([&](const Unit& u, int32_t from, int32_t to, int32_t seg) {
+                const int32_t h = SUMS ? u.head : u.head / prm.g, skip = SUMS ? first_q(u) : 0, per_head = prm.q_tiles - skip;
+                const int32_t k_slice = (prm.batch0 + u.b) * prm.kv_heads + h, q_slice0 = (prm.batch0 + u.b) * heads_q;
+                for (int32_t t = from; t < to; ++t, ++n) {
+                    const int s = (int)(n % STAGES);
+                    if (n >= STAGES && !mbar_wait(b_empty(s), (n / STAGES - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) return false;
+                    if (SUMS)
+                        load_operand(base + OFF_B + s * OPERAND, &map_q, b_full(s), (skip + t % per_head) * T, q_slice0 + h * prm.g + t / per_head);
+                    else
+                        load_operand(base + OFF_B + s * OPERAND, &map_k, b_full(s), t * T, k_slice);
+                    if (t == from) {  // the resident rows, when the products of the unit before are done with theirs
+                        if (seg > 0 && !mbar_wait(a_empty, (uint32_t)(seg - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) return false;
+                        if (SUMS)
+                            load_operand(base + OFF_A, &map_k, a_full, u.tile * T, k_slice);
+                        else
+                            load_operand(base + OFF_A, &map_q, a_full, u.tile * T, q_slice0 + u.head);
+                    }
+                }
+                return true;
+            });
             if (*abort_flag) {  // let the copies in flight land before this CTA's shared memory goes away
                 const unsigned long long t0 = global_timer_ns();
                 while (global_timer_ns() - t0 < LANDING_NS) __nanosleep(1000);
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && mbar_wait(a_full, 0, abort_flag, prm.status, prm.wait_limit_ns)) {
-            for (int32_t t = 0; t < n_tiles; ++t) {
-                const int s = t % STAGES, d = t & 1;
-                if (!mbar_wait(b_full(s), (uint32_t)(t / STAGES) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
-                if (t >= 2 && !mbar_wait(d_free(d), ((uint32_t)(t / 2) - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t aa = base + OFF_A, ba = base + OFF_B + s * OPERAND;
+        if (lane == 0) {
+            uint32_t n = 0;
+            segments([&](const Unit&, int32_t from, int32_t to, int32_t seg) {
+                if (!mbar_wait(a_full, (uint32_t)seg & 1, abort_flag, prm.status, prm.wait_limit_ns)) return false;
+                for (int32_t t = from; t < to; ++t, ++n) {
+                    const int s = (int)(n % STAGES), d = (int)(n & 1);
+                    if (!mbar_wait(b_full(s), (n / STAGES) & 1, abort_flag, prm.status, prm.wait_limit_ns)) return false;
+                    if (n >= 2 && !mbar_wait(d_free(d), (n / 2 - 1) & 1, abort_flag, prm.status, prm.wait_limit_ns)) return false;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t aa = base + OFF_A, ba = base + OFF_B + s * OPERAND;
 #pragma unroll
-                for (int part = 0; part < 3; ++part) {  // lo hi, hi lo, hi hi: the small ones first
-                    const uint32_t a_at = aa + (part == 0 ? 2 * SLAB : 0), b_at = ba + (part == 1 ? 2 * SLAB : 0);
+                    for (int part = 0; part < 3; ++part) {  // lo hi, hi lo, hi hi: the small ones first
+                        const uint32_t a_at = aa + (part == 0 ? 2 * SLAB : 0), b_at = ba + (part == 1 ? 2 * SLAB : 0);
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        umma(tmem_base + d * T, smem_desc(a_at + (kk / 4) * SLAB + (kk % 4) * 32, 16, 1024),
-                             smem_desc(b_at + (kk / 4) * SLAB + (kk % 4) * 32, 16, 1024), IDESC, (part | kk) != 0);
+                        for (int kk = 0; kk < 8; ++kk)
+                            umma(tmem_base + d * T, smem_desc(a_at + (kk / 4) * SLAB + (kk % 4) * 32, 16, 1024),
+                                 smem_desc(b_at + (kk / 4) * SLAB + (kk % 4) * 32, 16, 1024), IDESC, (part | kk) != 0);
+                    }
+                    umma_commit(d_full(d));
+                    umma_commit(b_empty(s));
                 }
-                umma_commit(d_full(d));
-                umma_commit(b_empty(s));
-            }
+                umma_commit(a_empty);
+                return true;
+            });
         }
     } else {
         const int quarter = warp % 4, half = (warp - 2) / 4, row = quarter * 32 + lane;  // tensor-memory lane = row of A
-        const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 64;
+        const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 64;
         const float c = prm.c;
-        float m = -1.0e30f;                       // pass 2: running maximum (of scores) and sum
-        float total[4] = {0.f, 0.f, 0.f, 0.f};    // pass 2: the sum in [0]; pass 3: four chains of the row's weight
+        uint32_t n = 0;
         bool alive = true;
-        for (int32_t t = 0; t < n_tiles; ++t) {
-            const int d = t & 1;
-            // pass 3: the maxima and sums of the tile's queries
-            const int32_t q0 = SUMS ? (first_tile + t % per_head) * T + half * 64 : 0;
-            const float2* stats = SUMS ? prm.stats + (int64_t)(q_slice0 + h * prm.g + t / per_head) * prm.n_pad + q0 : nullptr;
-            if (!mbar_wait(d_full(d), (uint32_t)(t / 2) & 1, abort_flag, prm.status, prm.wait_limit_ns)) {
-                alive = false;
-                break;
+        segments([&](const Unit& u, int32_t from, int32_t to, int32_t seg) {
+            const int32_t len = prm.len[u.b], pos0 = len - prm.n_new, row0 = u.tile * T, warp_row = row0 + quarter * 32;
+            const int32_t skip = SUMS ? first_q(u) : 0, per_head = prm.q_tiles - skip, q_slice0 = (prm.batch0 + u.b) * heads_q;
+            float m = -1.0e30f;                       // pass 2: running maximum (of scores) and sum
+            float total[4] = {0.f, 0.f, 0.f, 0.f};    // pass 2: the sum in [0]; pass 3: four chains of the row's weight
+            for (int32_t t = from; t < to && alive; ++t, ++n) {
+                const int d = (int)(n & 1);
+                // pass 3: the maxima and sums of the tile's queries
+                const int32_t q0 = SUMS ? (skip + t % per_head) * T + half * 64 : 0;
+                const float2* stats = SUMS ? prm.stats + (int64_t)(q_slice0 + u.head * prm.g + t / per_head) * prm.n_pad + q0 : nullptr;
+                if (!mbar_wait(d_full(d), (n / 2) & 1, abort_flag, prm.status, prm.wait_limit_ns)) {
+                    alive = false;
+                    break;
+                }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                uint32_t sc[64];
+                tmem_ld32<0>(lanes + d * T, sc);
+                tmem_ld32<32>(lanes + d * T + 32, sc);
+                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(d_free(d));
+                if constexpr (SUMS) {
+                    if (pos0 + q0 < warp_row + 31) {  // some queries come before some keys of this warp: those do not see them
+#pragma unroll
+                        for (int j = 0; j < 64; ++j)
+                            if (row0 + row > pos0 + q0 + j) sc[j] = __float_as_uint(-INFINITY);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 64; j += 2) {
+                        const float4 st = load(reinterpret_cast<const float4*>(stats + j));
+                        total[j / 2 & 3] = fmaf(ex2(fmaf(__uint_as_float(sc[j]), c, -st.x)), st.y, total[j / 2 & 3]);
+                        total[j / 2 & 3] = fmaf(ex2(fmaf(__uint_as_float(sc[j + 1]), c, -st.z)), st.w, total[j / 2 & 3]);
+                    }
+                } else {
+                    const int32_t j0 = t * T + half * 64, pos = pos0 + row0 + row;
+                    if (j0 + 63 > pos0 + warp_row) {
+#pragma unroll
+                        for (int j = 0; j < 64; ++j)
+                            if (j0 + j > pos) sc[j] = __float_as_uint(-INFINITY);
+                    }
+                    float m4[4] = {m, m, m, m};
+#pragma unroll
+                    for (int j = 0; j < 64; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], __uint_as_float(sc[j]), __uint_as_float(sc[j + 1]));
+                    const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                    // (the maximum as multiplied and rounded: where it has not changed the factor is one, not 2^(the product's rounding) for each tile)
+                    const float mc = __fmul_rn(mx, c);
+                    float s4[4] = {total[0] * ex2(__fmul_rn(m, c) - mc), 0.f, 0.f, 0.f};
+                    m = mx;
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) s4[j & 3] += ex2(fmaf(__uint_as_float(sc[j]), c, -mc));
+                    total[0] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                }
             }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            uint32_t sc[64];
-            tmem_ld32<0>(from + d * T, sc);
-            tmem_ld32<32>(from + d * T + 32, sc);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(d_free(d));
-            if constexpr (SUMS) {
-                const int32_t key = row0 + row;
-                if (pos0 + q0 < row0 + quarter * 32 + 31) {  // some queries come before some keys of this warp: those do not see them
-#pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if (key > pos0 + q0 + j) sc[j] = __float_as_uint(-INFINITY);
+            // the halves together, then the unit's result, or the share's part of it
+            float2* theirs = sm_half + (seg & 1) * T + row;
+            if (half == 1) *theirs = SUMS ? make_float2((total[0] + total[1]) + (total[2] + total[3]), 0.f) : make_float2(__fmul_rn(m, c), total[0]);
+            asm volatile("bar.sync 1, %0;" ::"r"(32 * READERS) : "memory");
+            if (half == 0 && alive) {
+                const float2 o = *theirs;
+                const bool whole = from == 0 && to == u.tiles;
+                float2* slot = prm.slots + (int64_t)(2 * share + (seg > 0)) * T + row;
+                if constexpr (SUMS) {
+                    const float sum = (total[0] + total[1]) + (total[2] + total[3]) + o.x;
+                    if (!whole)
+                        *slot = make_float2(sum, 0.f);
+                    else if (row0 + row < len)
+                        prm.mass[(int64_t)(prm.batch0 + u.b) * prm.mass_batch + u.head * prm.mass_rows + row0 + row] += sum;
+                } else {
+                    const float mine = __fmul_rn(m, c), mc = fmaxf(mine, o.x), l = total[0] * ex2(mine - mc) + o.y * ex2(o.x - mc);
+                    if (!whole)
+                        *slot = make_float2(mc, l);
+                    else  // queries past the chunk's last one: no weight
+                        prm.stats[(int64_t)(q_slice0 + u.head) * prm.n_pad + row0 + row] = row0 + row < prm.n_new ? make_float2(mc, 1.f / l) : make_float2(0.f, 0.f);
                 }
-#pragma unroll
-                for (int j = 0; j < 64; j += 2) {
-                    const float4 st = load(reinterpret_cast<const float4*>(stats + j));
-                    total[j / 2 & 3] = fmaf(ex2(fmaf(__uint_as_float(sc[j]), c, -st.x)), st.y, total[j / 2 & 3]);
-                    total[j / 2 & 3] = fmaf(ex2(fmaf(__uint_as_float(sc[j + 1]), c, -st.z)), st.w, total[j / 2 & 3]);
-                }
-            } else {
-                const int32_t j0 = t * T + half * 64, pos = pos0 + row0 + row;
-                if (j0 + 63 > pos0 + row0 + quarter * 32) {
-#pragma unroll
-                    for (int j = 0; j < 64; ++j)
-                        if (j0 + j > pos) sc[j] = __float_as_uint(-INFINITY);
-                }
-                float m4[4] = {m, m, m, m};
-#pragma unroll
-                for (int j = 0; j < 64; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], __uint_as_float(sc[j]), __uint_as_float(sc[j + 1]));
-                const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-                // (the maximum as multiplied and rounded: where it has not changed the factor is one, not 2^(the product's rounding) for each tile)
-                const float mc = __fmul_rn(mx, c);
-                float s4[4] = {total[0] * ex2(__fmul_rn(m, c) - mc), 0.f, 0.f, 0.f};
-                m = mx;
-#pragma unroll
-                for (int j = 0; j < 64; ++j) s4[j & 3] += ex2(fmaf(__uint_as_float(sc[j]), c, -mc));
-                total[0] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
             }
-        }
-        if (half == 1) sm_half[row] = SUMS ? make_float2((total[0] + total[1]) + (total[2] + total[3]), 0.f) : make_float2(m, total[0]);
-        asm volatile("bar.sync 1, %0;" ::"r"(32 * READERS) : "memory");
-        if (half == 0 && alive) {
-            const float2 o = sm_half[row];
-            if constexpr (SUMS) {
-                if (row0 + row < len) {
-                    float* at = prm.mass + (int64_t)(prm.batch0 + b) * prm.mass_batch + h * prm.mass_rows + row0 + row;
-                    *at += (total[0] + total[1]) + (total[2] + total[3]) + o.x;
-                }
-            } else {
-                const float mc = __fmul_rn(fmaxf(m, o.x), c), l = total[0] * ex2(__fmul_rn(m, c) - mc) + o.y * ex2(__fmul_rn(o.x, c) - mc);
-                // queries past the chunk's last one: no weight
-                prm.stats[(int64_t)(q_slice0 + q_head) * prm.n_pad + row0 + row] = row0 + row < prm.n_new ? make_float2(mc, 1.f / l) : make_float2(0.f, 0.f);
-            }
-        }
+            return true;  // having given up, too: every reader comes to every unit's barrier
+        });
     }
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -309,21 +392,65 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     }
 }
 
+// What several shares have of a unit, put together.  Block c has the unit that begins within share c and ends behind it, if there is one.
+template <bool SUMS>
+__global__ void __launch_bounds__(T) mass_join_kernel(const __grid_constant__ ChunkParams p)
+{
+    const int32_t share = (int32_t)blockIdx.x, row = (int32_t)threadIdx.x;
+    const uint64_t total = p.before[p.batch_count], begin = share_begin(total, p.shares, share), end = share_begin(total, p.shares, share + 1);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int32_t at;
+    const Unit u = find_unit<SUMS>(p, end - 1, at);
+    const uint64_t unit_begin = end - 1 - (uint32_t)at, unit_end = unit_begin + (uint32_t)u.tiles;
+    if (unit_end <= end || unit_begin < begin) return;
+    const int32_t last = share_of(total, p.shares, unit_end - 1);
+    // its first part: this share's last segment (its only one if it begins with the unit), then the others' first ones
+    float2 sum = p.slots[(int64_t)(2 * share + (unit_begin > begin)) * T + row];
+    for (int32_t s = share + 1; s <= last; ++s) {
+        const float2 o = p.slots[(int64_t)(2 * s) * T + row];
+        if (SUMS) {
+            sum.x += o.x;
+        } else {
+            const float mc = fmaxf(sum.x, o.x);
+            sum = make_float2(mc, sum.y * ex2(sum.x - mc) + o.y * ex2(o.x - mc));
+        }
+    }
+    const int32_t at_row = u.tile * T + row;
+    if (SUMS) {
+        if (at_row < p.len[u.b]) p.mass[(int64_t)(p.batch0 + u.b) * p.mass_batch + u.head * p.mass_rows + at_row] += sum.x;
+    } else {
+        p.stats[(int64_t)((p.batch0 + u.b) * heads_of<false>(p) + u.head) * p.n_pad + at_row] = at_row < p.n_new ? make_float2(sum.x, 1.f / sum.y) : make_float2(0.f, 0.f);
+    }
+}
+
 int32_t padded(int32_t n_new) { return (n_new + T - 1) / T * T; }
 
 }  // namespace
 
 size_t mass_key_bytes(const freqkv_layout& l) { return (size_t)l.batch * l.kv_heads * l.capacity * 512; }
 
-size_t mass_query_bytes(const freqkv_layout& l, int32_t q_heads_per_kv, int32_t n_new)
+size_t mass_query_bytes(const freqkv_layout& l, int32_t q_heads_per_kv, int32_t n_new, int sm_count)
 {
-    return (size_t)l.batch * l.kv_heads * q_heads_per_kv * ((size_t)n_new * 512 + (size_t)padded(n_new) * sizeof(float2));
+    return (size_t)l.batch * l.kv_heads * q_heads_per_kv * ((size_t)n_new * 512 + (size_t)padded(n_new) * sizeof(float2)) + (size_t)sm_count * 2 * T * sizeof(float2);
+}
+
+// The pass's shares: four tiles each at least.
+template <bool SUMS>
+static void share_out(ChunkParams& p, int sm_count)
+{
+    p.before[0] = 0;
+    for (int32_t b = 0; b < p.batch_count; ++b) {
+        uint64_t tiles = 0;
+        for (int32_t t = 0; t < row_tiles<SUMS>(p, b); ++t) tiles += (uint32_t)tiles_of<SUMS>(p, b, t);
+        p.before[b + 1] = p.before[b] + tiles * (uint32_t)heads_of<SUMS>(p);
+    }
+    p.shares = (int32_t)std::min<uint64_t>((uint64_t)sm_count, (p.before[p.batch_count] + 3) / 4);
 }
 
 cudaError_t launch_attend_chunk_mass(const freqkv_layout& l, const void* k, int32_t layer, const void* q, float* mass, int32_t g, int32_t n_new,
                                      const int32_t* lens_host, const float2* table, float scale, void* key_scratch, void* query_scratch,
-                                     int32_t* status, unsigned long long wait_limit_ns, const char** error, int32_t* kernels_launched,
-                                     cudaStream_t stream)
+                                     int sm_count, int32_t* status, unsigned long long wait_limit_ns, const char** error,
+                                     int32_t* kernels_launched, cudaStream_t stream)
 {
     *error = nullptr;
     if (!encode_fn()) {
@@ -382,30 +509,35 @@ cudaError_t launch_attend_chunk_mass(const freqkv_layout& l, const void* k, int3
         prm.batch0 = b0;
         prm.batch_count = nb;
         prm.q_tiles = prm.n_pad / T;
-        prm.k_tiles = (max_len + T - 1) / T;
         prm.c = scale * 1.4426950408889634f;
         prm.stats = reinterpret_cast<float2*>(queries + (int64_t)l.batch * heads_q * n_new * 256);
+        prm.slots = prm.stats + (int64_t)l.batch * heads_q * prm.n_pad;
         prm.mass = mass + (int64_t)layer * l.kv_heads * l.capacity;
         prm.mass_batch = (int64_t)l.layers * l.kv_heads * l.capacity;
         prm.mass_rows = l.capacity;
         prm.status = status;
         prm.wait_limit_ns = wait_limit_ns;
-        cudaLaunchConfig_t cfg = {};
-        cfg.blockDim = dim3(THREADS);
-        cfg.dynamicSmemBytes = SMEM_BYTES;
-        cfg.stream = stream;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;  // let each launch overlap the tail of the one before
-        attr.val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        cfg.gridDim = dim3((unsigned)((int64_t)prm.q_tiles * heads_q * nb));
-        e = cudaLaunchKernelEx(&cfg, mass_tiles_kernel<false>, map_q, map_k, prm);
+        auto launch = [&](auto* kernel, int threads, int smem, auto... args) {  // each may overlap the tail of the one before
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)prm.shares);
+            cfg.blockDim = dim3((unsigned)threads);
+            cfg.dynamicSmemBytes = (size_t)smem;
+            cfg.stream = stream;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr.val.programmaticStreamSerializationAllowed = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            return cudaLaunchKernelEx(&cfg, kernel, args...);
+        };
+        share_out<false>(prm, sm_count);
+        e = launch(mass_tiles_kernel<false>, THREADS, SMEM_BYTES, map_q, map_k, prm);
+        if (e == cudaSuccess) e = launch(mass_join_kernel<false>, T, 0, prm);
+        share_out<true>(prm, sm_count);
+        if (e == cudaSuccess) e = launch(mass_tiles_kernel<true>, THREADS, SMEM_BYTES, map_q, map_k, prm);
+        if (e == cudaSuccess) e = launch(mass_join_kernel<true>, T, 0, prm);
         if (e != cudaSuccess) return e;
-        cfg.gridDim = dim3((unsigned)((int64_t)prm.k_tiles * l.kv_heads * nb));
-        e = cudaLaunchKernelEx(&cfg, mass_tiles_kernel<true>, map_q, map_k, prm);
-        if (e != cudaSuccess) return e;
-        *kernels_launched += 3;
+        *kernels_launched += 5;
     }
     return cudaSuccess;
 }
