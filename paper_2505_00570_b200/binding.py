@@ -272,7 +272,7 @@ class Q8Cache:
         if not k.device == v.device == k_scale.device == v_scale.device:
             raise FreqKVError(ERR_INVALID_ARG, "codes and scales must be on one device")
         self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
-        self.layout, self._ref = ref
+        self.layout, self._ref, self._dims = ref
         self._ptrs = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
 
     @staticmethod
@@ -291,7 +291,7 @@ class Q8Cache:
             if s.dtype != torch.float32 or tuple(s.shape) != want or not s.is_contiguous():
                 raise FreqKVError(ERR_INVALID_ARG, f"scales must be dense fp32 {want}")
         layout = Q8Layout(kinds[k.dtype], *k.shape, block_tokens, *k.stride()[:4])
-        return layout, ctypes.byref(layout)
+        return layout, ctypes.byref(layout), (layout.batch, layout.kv_heads, layout.head_dim)
 
     @classmethod
     def empty(cls, batch: int, layers: int, kv_heads: int, capacity: int, head_dim: int = 128, kind: int = Q8_E4M3,
@@ -539,13 +539,17 @@ class Context:
                          scale: float = 0.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """``attend_decode`` over an 8-bit cache.  ``q``: dense bf16 [batch, q_heads, 128], before RoPE; q_heads a multiple (at
         most 64 times) of the cache's kv_heads.  Returns ``out``."""
-        lay = cache.layout
-        if q.dim() != 3 or not q.is_contiguous() or q.dtype != torch.bfloat16 or q.shape[0] != lay.batch or \
-                q.shape[2] != lay.head_dim or q.shape[1] % lay.kv_heads != 0 or len(lens) != lay.batch:
+        batch, kv_heads, head_dim = cache._dims
+        shape = q.shape
+        if len(shape) != 3 or shape[0] != batch or shape[2] != head_dim or shape[1] % kv_heads or q.dtype is not torch.bfloat16 or \
+                not q.is_contiguous() or len(lens) != batch:
             raise FreqKVError(ERR_INVALID_ARG, "q must be dense bf16 [batch, q_heads, head_dim], lens one entry per sequence")
-        out = self._out(q, out)
-        st = lib().freqkv_attend_decode_q8(self._h, cache._ref, *cache._ptrs, layer, q.data_ptr(), out.data_ptr(),
-                                           q.shape[1] // lay.kv_heads, (c_int32 * lay.batch)(*lens), rope_base, scale, _stream_ptr(stream))
+        if out is None:
+            out = torch.empty_like(q)
+        elif out.shape != shape or out.dtype is not torch.bfloat16 or not out.is_contiguous():
+            raise FreqKVError(ERR_INVALID_ARG, "out must be dense and like q")
+        st = lib().freqkv_attend_decode_q8(self._h, cache._ref, *cache._ptrs, layer, q.data_ptr(), out.data_ptr(), shape[1] // kv_heads,
+                                           (c_int32 * batch)(*lens), rope_base, scale, _stream_ptr(stream))
         self._check(st, "freqkv_attend_decode_q8")
         return out
 
