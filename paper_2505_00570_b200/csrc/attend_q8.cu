@@ -184,6 +184,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
     float4* sm_q = reinterpret_cast<float4*>(smem + OFF_Q);
     float* sm_o = reinterpret_cast<float*>(smem);  // after the loop
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, gq = lane / 4, tq = lane % 4;
+    const int32_t sub = (int32_t)blockIdx.y % p.subs, bh = (int32_t)blockIdx.y / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
+    const int32_t len = p.len[b];
+    const int32_t rows = p.tiles[b] * TILE, r0 = (int32_t)blockIdx.x * rows, r1 = min(len, r0 + rows);
+    if (r0 >= len) return;  // a shorter sequence has fewer splits
     if (!p.early) wait_for_previous_grid();
     // cosines and sines of rows 0 .. 63: they do not depend on the grid before this one once the table has been there for a while
     if (p.table) {
@@ -196,10 +200,6 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_q8_kernel(const _
         }
     }
     if (p.early) wait_for_previous_grid();
-    const int32_t sub = (int32_t)blockIdx.y % p.subs, bh = (int32_t)blockIdx.y / p.subs, b = bh / p.kv_heads, h = bh % p.kv_heads;
-    const int32_t len = p.len[b];
-    const int32_t rows = p.tiles[b] * TILE, r0 = (int32_t)blockIdx.x * rows, r1 = min(len, r0 + rows);
-    if (r0 >= len) return;  // a shorter sequence has fewer splits
     // each warp walks a run of tiles
     const int32_t n_tiles = (r1 - r0 + TILE - 1) / TILE, per = (n_tiles + WARPS - 1) / WARPS, t0 = min(n_tiles, warp * per), t1 = min(n_tiles, t0 + per);
     const int32_t heads = min(Q8_HEADS, p.g - sub * Q8_HEADS);

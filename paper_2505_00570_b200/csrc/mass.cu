@@ -267,10 +267,6 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
                 return true;
             });
-            if (*abort_flag) {  // let the copies in flight land before this CTA's shared memory goes away
-                const unsigned long long t0 = global_timer_ns();
-                while (global_timer_ns() - t0 < LANDING_NS) __nanosleep(1000);
-            }
         }
     } else if (warp == 1) {
         if (lane == 0) {
@@ -386,6 +382,11 @@ mass_tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (*abort_flag) {  // whichever role gave up: copies and products in flight land before shared and tensor memory go away
+        const unsigned long long t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < LANDING_NS) __nanosleep(1000);
+        __syncthreads();
+    }
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS));

@@ -404,10 +404,6 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                     tma_load_5d(base + OFF_V + sv * KV_TILE + KV_SLAB, &map_v, v_full(sv), 64, t * BKV, h, prm.layer, prm.batch0 + b);
                 }
             }
-            if (*abort_flag) {  // let the copies in flight land before this CTA's shared memory goes away
-                const unsigned long long t0 = global_timer_ns();
-                while (global_timer_ns() - t0 < LANDING_NS) __nanosleep(1000);
-            }
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
@@ -558,6 +554,11 @@ prefill_attend_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (*abort_flag) {  // whichever role gave up: copies and products in flight land before shared and tensor memory go away
+        const unsigned long long t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < LANDING_NS) __nanosleep(1000);
+        __syncthreads();
+    }
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS));

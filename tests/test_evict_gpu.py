@@ -277,6 +277,31 @@ def test_chunk_mass_captured_and_refused(ctx):
     assert torch.equal(mass, 2 * once)
 
 
+def test_weights_back_to_back_on_streams_in_turn(ctx):
+    """Layer after layer without a wait, streams in turn, decode and chunk calls that share the context's work areas: the sums of the calls
+    alone, bit for bit."""
+    k, v = caches(2, 3, 2, 1500, torch.bfloat16, 31)
+    one, chunk = queries((2, 8, 128), torch.bfloat16, 5), queries((2, 8, 150, 128), torch.bfloat16, 6)
+    lens = [1500, 160]
+    want = torch.zeros(2, 3, 2, 1500, device="cuda")
+    for layer in range(3):
+        ctx.attend_decode_mass(k, v, layer, one, want, lens)
+        torch.cuda.synchronize()
+        ctx.attend_mass(k, layer, chunk, want, lens)
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    for layer in range(3):
+        with torch.cuda.stream(streams[layer % 2]):
+            ctx.attend_decode_mass(k, v, layer, one, got, lens)
+        with torch.cuda.stream(streams[(layer + 1) % 2]):
+            ctx.attend_mass(k, layer, chunk, got, lens)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    assert ctx.last_device_status() == fk.OK
+
+
 # ---- eviction ----
 
 def check_evict(ctx, k, v, mass, lens, kept, sink, recent, in_place=True, with_rows=True):

@@ -182,6 +182,58 @@ def test_decode_many_sequences_and_captured(ctx):
     assert torch.equal(ctx.attend_decode_q8(cache, 0, q, lens), out)   # the same call gives the same bits
 
 
+def test_decode_ragged_lengths_in_many_splits_back_to_back(ctx):
+    """Sequences of one row beside long ones, layer after layer without a wait, bases in turn (each makes its table anew), other calls of
+    the context between them: every result is that of the call alone."""
+    cache = make(ctx, 3, 3, 2, 4000, "e4m3", 32, seed=15)
+    k, v = rows((3, 1, 2, 500, 128), torch.bfloat16, 3), rows((3, 1, 2, 500, 128), torch.bfloat16, 4)
+    q, lens = queries((3, 8, 128), 3), [1, 4000, 17]
+    alone = {}
+    for layer in range(3):
+        for base in (10000.0, 500000.0):
+            alone[layer, base] = ctx.attend_decode_q8(cache, layer, q, lens, rope_base=base).clone()
+            torch.cuda.synchronize()
+    kv = values(cache)
+    for layer in (0, 2):
+        check_decode(ctx, cache, layer, q, lens, kv=kv)
+    got = []
+    for _ in range(3):
+        for base in (10000.0, 500000.0):
+            for layer in range(3):
+                got.append((layer, base, ctx.attend_decode_q8(cache, layer, q, lens, rope_base=base)))
+            ctx.attend_decode(k, v, 0, q, [500, 3, 70], rope_base=base)
+    for layer, base, out in got:
+        assert torch.equal(out, alone[layer, base])
+
+
+def test_two_contexts_on_two_streams(ctx):
+    other = fk.Context(0)
+    a, b = make(ctx, 2, 1, 4, 3000, "e4m3", 64, seed=16), make(ctx, 2, 1, 4, 3000, "int8", 16, seed=17)
+    qa, qb = queries((2, 16, 128), 3), queries((2, 4, 128), 4)
+    chunk = queries((2, 16, 200, 128), 5)
+    want = [ctx.attend_decode_q8(a, 0, qa, [3000, 2000]), ctx.attend_decode_q8(b, 0, qb, [700, 3000]), ctx.attend_prefill_q8(a, 0, chunk, [3000, 777])]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(5):
+        with torch.cuda.stream(streams[0]):
+            x, z = ctx.attend_decode_q8(a, 0, qa, [3000, 2000]), ctx.attend_prefill_q8(a, 0, chunk, [3000, 777])
+        with torch.cuda.stream(streams[1]):
+            y = other.attend_decode_q8(b, 0, qb, [700, 3000])
+        got.append((x, y, z))
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(p, w) for p, w in zip(g, want))
+    # one context, streams in turn: its calls follow one another
+    outs = []
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            outs.append(ctx.attend_decode_q8(a, 0, qa, [3000, 2000]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[0]) for o in outs)
+    other.close()
+
+
 def test_decode_long_cache_and_offsets_past_32_bits(ctx):
     cap = 9_000_000                                    # 128 bytes a row: one matrix past 1 GB, the second head past 2^30 rows' bytes
     cache = fk.Q8Cache.empty(1, 2, 2, cap, 128, fk.Q8_INT8, 128)
