@@ -11,6 +11,10 @@
 // its own two-stage ring; a lane has 16 consecutive channels and the 16 that RoPE pairs with them of two key rows; keys are turned,
 // in fp32, by their row's place within 64 rows, queries by what is left, once in 64 rows.  Weights enter the second product
 // as two bf16 parts (16 bits), values as they lie in the cache.
+//
+// PAIRED: up to four query heads leave half of a product's eight columns empty; their lo parts take these, so that two products (and one of
+// values) do for three (and two): 8 sequences of 8 x 4 heads, 8 layers 436 -> 429 us.  Eight heads: PAIRED = false.
+// (One CTA of 10 to 12 warps instead of two of 4: 500 us and more, its splits fill the chip less evenly.)
 #include <algorithm>
 
 #include "attend_dev.cuh"
@@ -78,15 +82,23 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
     return y;
 }
-// Two fp16 parts of two values.
-__device__ __forceinline__ void split(float2 x, uint32_t& hi, uint32_t& lo)
+__device__ __forceinline__ f2 sub2(f2 a, f2 b)
 {
-    const __half2 h = __floats2half2_rn(x.x, x.y);
-    const float2 f = __half22float2(h);
+    f2 y;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+// Two fp16 parts of two values.
+__device__ __forceinline__ void split(f2 x, uint32_t& hi, uint32_t& lo)
+{
+    const float2 v = unpack(x);
+    const __half2 h = __floats2half2_rn(v.x, v.y);
+    const float2 f = __half22float2(h), d = unpack(sub2(x, pack(f.x, f.y)));
     hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = pack2_f16(x.x - f.x, x.y - f.y);
+    lo = pack2_f16(d.x, d.y);
 }
 
+template <bool PAIRED>
 __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(const __grid_constant__ ScoreParams p)
 {
     wait_for_previous_grid();
@@ -163,8 +175,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-    uint32_t qh[2][4][2], ql[2][4][2];  // [channels below, from 64][four channels][two pairs]: hi and lo parts
-    const int64_t score0 = (head0 + 2 * tq) * p.score_rows + gq;
+    uint32_t qh[2][4][2], ql[2][4][2];  // [channels below, from 64][four channels][two pairs]: hi and lo parts (PAIRED: qh has the column's)
+    const int column = PAIRED ? gq & 3 : gq, head = PAIRED ? 2 * (tq & 1) : 2 * tq;  // heads: of the queries' column; of this lane's two scores
+    const bool second = PAIRED && tq >= 2;                                          // the lane's columns are lo parts
+    const int64_t score0 = (head0 + head) * p.score_rows + gq;
 
     int stage = 0;
     for (int32_t tile = t0; tile < t1; ++tile, stage ^= 1) {
@@ -175,7 +189,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
             const float4* turn = reinterpret_cast<const float4*>(smem + OFF_TURN + warp * 512) + 8 * tq;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                float4 lo = sm_q[gq * Q_ROW + w * 4 + tq], hi = sm_q[gq * Q_ROW + 16 + w * 4 + tq];
+                float4 lo = sm_q[column * Q_ROW + w * 4 + tq], hi = sm_q[column * Q_ROW + 16 + w * 4 + tq];
                 if (p.table) {
                     const float4 c0 = turn[2 * w], c1 = turn[2 * w + 1];
                     rotate(lo.x, hi.x, make_float2(c0.x, c0.y));
@@ -183,10 +197,16 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
                     rotate(lo.z, hi.z, make_float2(c1.x, c1.y));
                     rotate(lo.w, hi.w, make_float2(c1.z, c1.w));
                 }
-                split(make_float2(lo.x, lo.y), qh[0][w][0], ql[0][w][0]);
-                split(make_float2(lo.z, lo.w), qh[0][w][1], ql[0][w][1]);
-                split(make_float2(hi.x, hi.y), qh[1][w][0], ql[1][w][0]);
-                split(make_float2(hi.z, hi.w), qh[1][w][1], ql[1][w][1]);
+                split(pack(lo.x, lo.y), qh[0][w][0], ql[0][w][0]);
+                split(pack(lo.z, lo.w), qh[0][w][1], ql[0][w][1]);
+                split(pack(hi.x, hi.y), qh[1][w][0], ql[1][w][0]);
+                split(pack(hi.z, hi.w), qh[1][w][1], ql[1][w][1]);
+                if (PAIRED && gq >= 4) {
+                    qh[0][w][0] = ql[0][w][0];
+                    qh[0][w][1] = ql[0][w][1];
+                    qh[1][w][0] = ql[1][w][0];
+                    qh[1][w][1] = ql[1][w][1];
+                }
             }
             __syncwarp();
             fetch_turn(tile + TURN_TILES);  // (with the next tile's group: there before it is read, three tiles on)
@@ -218,14 +238,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
                         const f2 hi = pack(__uint_as_float(uh << 16), __uint_as_float(uh & 0xffff0000u));
                         const f2 cc = i ? pack(c.z, c.w) : pack(c.x, c.y), ss = i ? pack(s.z, s.w) : pack(s.x, s.y);
                         const f2 minus = i ? pack(-s.z, -s.w) : pack(-s.x, -s.y);
-                        split(unpack(fma2(hi, minus, mul2(lo, cc))), ah[0][r + 2 * i], al[0][r + 2 * i]);
-                        split(unpack(fma2(lo, ss, mul2(hi, cc))), ah[1][r + 2 * i], al[1][r + 2 * i]);
+                        split(fma2(hi, minus, mul2(lo, cc)), ah[0][r + 2 * i], al[0][r + 2 * i]);
+                        split(fma2(lo, ss, mul2(hi, cc)), ah[1][r + 2 * i], al[1][r + 2 * i]);
                     }
                 }
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     mma_f16(big[x], ah[x], qh[x][w][0], qh[x][w][1]);
-                    mma_f16(small[x], ah[x], ql[x][w][0], ql[x][w][1]);
+                    if (!PAIRED) mma_f16(small[x], ah[x], ql[x][w][0], ql[x][w][1]);
                     mma_f16(small[x], al[x], qh[x][w][0], qh[x][w][1]);
                 }
             }
@@ -233,14 +253,22 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
         // this thread's rows gq and gq + 8; the scores go out in units of log2
         float pw[2][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pw[i / 2][i % 2] = ((small[0][i] + small[1][i]) + (big[0][i] + big[1][i])) * p.qscale;
+        for (int i = 0; i < 4; ++i) {
+            float s = (small[0][i] + small[1][i]) + (big[0][i] + big[1][i]);
+            if (PAIRED) s += __shfl_xor_sync(0xffffffffu, s, 2);  // the same sum in both lanes
+            pw[i / 2][i % 2] = s * p.qscale;
+        }
         const bool ok0 = j0 + gq < warp_end, ok1 = j0 + gq + 8 < warp_end;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-            if (2 * tq + j < heads) {
+            if (head + j < heads) {
                 float* at = p.scores + score0 + j * p.score_rows + j0;
-                if (ok0) at[0] = pw[0][j];
-                if (ok1) at[8] = pw[1][j];
+                if (PAIRED) {  // the lane of the hi parts writes row gq, the other one row gq + 8
+                    if (second ? ok1 : ok0) at[second ? 8 : 0] = second ? pw[1][j] : pw[0][j];
+                } else {
+                    if (ok0) at[0] = pw[0][j];
+                    if (ok1) at[8] = pw[1][j];
+                }
             }
         if (!ok0) pw[0][0] = pw[0][1] = -INFINITY;
         if (!ok1) pw[1][0] = pw[1][1] = -INFINITY;
@@ -276,8 +304,9 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const uint32_t hi = pack2_bf16(pw[r][0], pw[r][1]);
-            pl[r] = transpose_8x8(pack2_bf16(pw[r][0] - __uint_as_float(hi << 16), pw[r][1] - __uint_as_float(hi & 0xffff0000u)));
-            ph[r] = transpose_8x8(hi);
+            const uint32_t lo = pack2_bf16(pw[r][0] - __uint_as_float(hi << 16), pw[r][1] - __uint_as_float(hi & 0xffff0000u));
+            if (!PAIRED) pl[r] = transpose_8x8(lo);
+            ph[r] = transpose_8x8(second ? lo : hi);
         }
         // O^T += V^T P: product i takes channels 16 gq + 2 i and + 1
 #pragma unroll
@@ -288,7 +317,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
             for (int i = 0; i < 4; ++i) {
                 const uint32_t v0 = word(v[0], i), v1 = word(v[1], i), v2 = word(v[2], i), v3 = word(v[3], i);
                 const uint32_t a[4] = {__byte_perm(v0, v1, 0x5410), __byte_perm(v0, v1, 0x7632), __byte_perm(v2, v3, 0x5410), __byte_perm(v2, v3, 0x7632)};
-                mma_bf16(o[4 * w2 + i], a, pl[0], pl[1]);
+                if (!PAIRED) mma_bf16(o[4 * w2 + i], a, pl[0], pl[1]);
                 mma_bf16(o[4 * w2 + i], a, ph[0], ph[1]);
             }
         }
@@ -302,12 +331,12 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
         l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 4);
         l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 8);
         l_run[j] += __shfl_xor_sync(0xffffffffu, l_run[j], 16);
-        const int head = 2 * tq + j;
+        const int col = 2 * tq + j;  // PAIRED: of the lo parts from HEADS / 2 on
         if (gq == 0) {
-            sm_ml[warp][head][0] = m_run[j];
-            sm_ml[warp][head][1] = l_run[j];
+            sm_ml[warp][col][0] = m_run[j];
+            sm_ml[warp][col][1] = l_run[j];
         }
-        float* at = sm_o + (warp * HEADS + head) * O_ROW + gq;
+        float* at = sm_o + (warp * HEADS + col) * O_ROW + gq;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             at[16 * i] = o[i][j];
@@ -323,7 +352,8 @@ __global__ void __launch_bounds__(THREADS, CTAS_PER_SM) attend_scores_kernel(con
         for (int w = 0; w < WARPS; ++w) {
             const float f = ex2(sm_ml[w][g][0] - mn);
             sum = fmaf(sm_ml[w][g][1], f, sum);
-            acc = fmaf(sm_o[(w * HEADS + g) * O_ROW + tid], f, acc);
+            const float* at = sm_o + (w * HEADS + g) * O_ROW + tid;
+            acc = fmaf(PAIRED ? at[0] + at[HEADS / 2 * O_ROW] : at[0], f, acc);
         }
         float* part = p.partial + (((int64_t)blockIdx.x * p.total_batch + bb) * p.kv_heads * p.g + h * p.g + g) * PART;
         part[4 + tid] = acc;
@@ -344,8 +374,11 @@ cudaError_t launch_attend_scores(const freqkv_layout& l, const void* k, const vo
 {
     static PerDeviceOnce attrs;
     const cudaError_t attr_error = attrs.run([] {
-        cudaError_t e = cudaFuncSetAttribute(attend_scores_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_scores_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        cudaError_t e = cudaSuccess;
+        for (auto* kernel : {attend_scores_kernel<false>, attend_scores_kernel<true>}) {
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        }
         return e;
     });
     if (attr_error != cudaSuccess) return attr_error;
@@ -379,7 +412,7 @@ cudaError_t launch_attend_scores(const freqkv_layout& l, const void* k, const vo
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = overlap ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, attend_scores_kernel, prm);
+    return cudaLaunchKernelEx(&cfg, g <= HEADS / 2 ? attend_scores_kernel<true> : attend_scores_kernel<false>, prm);
 }
 
 }  // namespace freqkv
